@@ -412,6 +412,81 @@ gt_status gt_feature_code_table(const float* weights, const uint32_t* vectors, i
 gt_status gt_feature_code_dweights(const float* dtable, const uint32_t* vectors, int32_t n_heads, int32_t n_codes,
                                    float* dweights, void* stream);
 
+/* ---------------------------------------------------------------------------------------
+ * gt_position_attn_fwd / gt_position_attn_bwd -- attention over token SEQUENCES: the structure of a batch is the order of its
+ * rows, so no SPD matrix is built or read (for a sequence the distance of two nodes is |i - j|).  The batch's graphs are
+ * documents: document g owns rows cu_seqlens[g] .. cu_seqlens[g+1]-1 (none, one or more), a row's position i is its index in its
+ * document, and with x_ij = (q_i . k_j)/sqrt(head_dim)
+ *     S_ij = (cap > 0 ? cap * tanh(x_ij / cap) : x_ij) - slopes[h] * |i - j|          (slopes NULL: no such term)
+ *     out_i = sum_j softmax_j(S_i)_j v_j,     lse[h][i] = log sum_j exp(S_ij)
+ * over the keys j that i sees: all of its document (causal == 0), or j <= i and j < prefix[g] (causal != 0; prefix int32[G] on the
+ * device, any values, NULL: zeros; with causal == 0 prefix must be NULL).  Every query sees itself.
+ * q bf16 [T, n_heads, d]; k, v bf16 [T, n_kv_heads, d], n_kv_heads dividing n_heads: query head h reads key head
+ * h / (n_heads / n_kv_heads).  slopes: fp32 [n_heads], constants of the model (they get no gradient).  cap: 0, or 1e-6 .. 1e6.
+ * strides (host, NULL: packed): elements from a row of q, k, v (bwd: and of dq, dk, dv) to the next, 0 for a packed tensor, each
+ * a multiple of 8; so q, k and v may be parts of the rows of one projection.  out, dout and lse ([n_heads, T]) are packed.
+ * Rows behind the last document (cu_seqlens[G] < n_total) belong to none: their results are left as they were.
+ * One document's values never reach another's results.  Within a document a NaN or an infinity in k or v may reach queries that
+ * do not see it (they meet it multiplied by zero), as may one in q or dout reach gradients.
+ *
+ * The backward takes out and lse of the forward with the same arguments.  With P = exp(S - lse), Delta_i = dout_i . out_i:
+ *     dv_j = sum P_ij dout_i,   dS_ij = P_ij (dout_i . v_j - Delta_i) (1 - tanh^2(x_ij / cap)),
+ *     dq_i = sum_j dS_ij k_j / sqrt(d),   dk_j = sum dS_ij q_i / sqrt(d),
+ * dk and dv summed over the query heads that share a key head.  dq, dk, dv (bf16) are overwritten; they must not overlap any
+ * input.  dq, and with shared key heads dk and dv, are accumulated with floating-point atomics in fp32: their low-order bits may
+ * differ from run to run.
+ * Workspace as for every call (header zero at first).  Forward: 256 bytes and 16 per document and per 256 rows; backward:
+ * (4 d + 32) bytes per row and query head, 8 d per row and key head where heads share keys, and 16 per document and 128 rows.
+ * A query with bad arguments returns 0.
+ * ------------------------------------------------------------------------------------- */
+typedef struct gt_row_strides {
+    int64_t q, k, v;           /* inputs                       */
+    int64_t dq, dk, dv;        /* gradients (backward only)    */
+} gt_row_strides;
+
+size_t gt_position_attn_fwd_workspace(const gt_batch* batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
+gt_status gt_position_attn_fwd(const void* q, const void* k, const void* v, const float* slopes, const int32_t* prefix,
+                               const gt_batch* batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                               const gt_row_strides* strides, int32_t causal, float cap, void* out, float* lse,
+                               void* workspace, size_t workspace_bytes, void* stream);
+size_t gt_position_attn_bwd_workspace(const gt_batch* batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
+gt_status gt_position_attn_bwd(const void* q, const void* k, const void* v, const void* out, const void* dout, const float* lse,
+                               const float* slopes, const int32_t* prefix,
+                               const gt_batch* batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                               const gt_row_strides* strides, int32_t causal, float cap,
+                               void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * gt_rotary -- rotary positions of the queries and keys of gt_position_attn_*: pair i of a head's first rot_dim channels, (a, b) at
+ * position p, becomes
+ *     scale * (a cos w - b sin w, a sin w + b cos w),      w = p * frequencies[i]
+ * (inverse != 0: w negated: the transpose, which takes the gradients dq and dk of the rotated rows to those of the rows).
+ * interleaved != 0: the pairs are channels (2 i, 2 i + 1); 0: (i, i + rot_dim / 2).  The other channels stay as they are.
+ * q [T, n_heads, head_dim] and k [T, n_kv_heads, head_dim] of type dtype (k and k_out NULL and n_kv_heads 0: q only), rows
+ * *_stride elements apart (0: packed); q_out, k_out likewise.  An output may be its input (same address, same stride); otherwise
+ * outputs must not overlap inputs.  positions: int32 [T] on the device, any values, or NULL: a row's index in its document.
+ * frequencies: fp64 [rot_dim / 2] on the device, radians per position; rot_dim even, 2 .. head_dim; head_dim 32 or 64.
+ * Angles are reduced in fp64 (within 5e-7 rad at 2^31 positions x 1 rad), results rounded once.  Rows behind the last document
+ * are left as they were.  Rows at 16-byte addresses and strides, and with the halves 2 * 16 bytes' worth of rot_dim, are fastest;
+ * any other element's address is taken, too.  No workspace.
+ *
+ * gt_rotary_frequencies -- the table, into HOST memory (fp64 [rot_dim / 2]): f_i = base^(-2 i / rot_dim), for contexts longer than
+ * the trained one scaled by `factor`:  GT_ROTARY_LINEAR f_i / factor;  GT_ROTARY_BASE base * factor^(rot_dim / (rot_dim - 2)) in
+ * place of base;  GT_ROTARY_PARTS f_i ((1 - c) / factor + c), where c rises from 0 to 1 as the turns that f_i makes within
+ * original_length, original_length f_i / 2 pi, go from low to high (arXiv 2309.00071, Sec. 3.2; a factor on the scores goes into
+ * `scale` of gt_rotary).  What a scaling does not use is ignored.
+ * ------------------------------------------------------------------------------------- */
+typedef enum gt_dtype { GT_BF16 = 0, GT_FP16 = 1, GT_FP32 = 2 } gt_dtype;
+typedef enum gt_rotary_scaling { GT_ROTARY_PLAIN = 0, GT_ROTARY_LINEAR = 1, GT_ROTARY_BASE = 2, GT_ROTARY_PARTS = 3 } gt_rotary_scaling;
+
+gt_status gt_rotary(const void* q, const void* k, const double* frequencies, const int32_t* positions,
+                    const gt_batch* batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t rot_dim,
+                    gt_dtype dtype, int32_t interleaved, float scale, int32_t inverse,
+                    int64_t q_stride, int64_t k_stride, int64_t q_out_stride, int64_t k_out_stride,
+                    void* q_out, void* k_out, void* stream);
+gt_status gt_rotary_frequencies(int32_t rot_dim, double base, gt_rotary_scaling scaling, double factor,
+                                double original_length, double low, double high, double* frequencies_host);
+
 #ifdef __cplusplus
 }
 #endif

@@ -33,7 +33,12 @@ EXPORTS = ("gt_status_string", "gt_check",
            "gt_biased_attn_bwd_step", "gt_biased_attn_bwd_step_finish",
            "gt_feature_attn_fwd", "gt_feature_attn_bwd_workspace", "gt_feature_attn_bwd",
            "gt_feature_encode_workspace", "gt_feature_encode", "gt_feature_encode_count",
-           "gt_feature_code_table", "gt_feature_code_dweights")
+           "gt_feature_code_table", "gt_feature_code_dweights",
+           "gt_position_attn_fwd_workspace", "gt_position_attn_fwd",
+           "gt_position_attn_bwd_workspace", "gt_position_attn_bwd",
+           "gt_rotary", "gt_rotary_frequencies")
+DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+ROTARY_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
 
 
 class GtError(RuntimeError):
@@ -45,6 +50,10 @@ class GtError(RuntimeError):
 class _GtBatch(ctypes.Structure):
     _fields_ = [("n_total", ctypes.c_int32), ("n_graphs", ctypes.c_int32),
                 ("cu_seqlens", ctypes.c_void_p), ("max_seqlen", ctypes.c_int32)]
+
+
+class _GtRowStrides(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("q", "k", "v", "dq", "dk", "dv")]
 
 
 _lib = None
@@ -132,6 +141,19 @@ def lib() -> ctypes.CDLL:
         L.gt_feature_code_table.argtypes = [vp, vp, i32, i32, vp, vp]
         L.gt_feature_code_dweights.restype = ctypes.c_int
         L.gt_feature_code_dweights.argtypes = [vp, vp, i32, i32, vp, vp]
+        f32, f64, sp = ctypes.c_float, ctypes.c_double, ctypes.POINTER(_GtRowStrides)
+        L.gt_position_attn_fwd_workspace.restype = sz
+        L.gt_position_attn_fwd_workspace.argtypes = [bp, i32, i32, i32]
+        L.gt_position_attn_fwd.restype = ctypes.c_int
+        L.gt_position_attn_fwd.argtypes = [vp] * 5 + [bp, i32, i32, i32, sp, i32, f32, vp, vp, vp, sz, vp]
+        L.gt_position_attn_bwd_workspace.restype = sz
+        L.gt_position_attn_bwd_workspace.argtypes = [bp, i32, i32, i32]
+        L.gt_position_attn_bwd.restype = ctypes.c_int
+        L.gt_position_attn_bwd.argtypes = [vp] * 8 + [bp, i32, i32, i32, sp, i32, f32, vp, vp, vp, vp, sz, vp]
+        L.gt_rotary.restype = ctypes.c_int
+        L.gt_rotary.argtypes = [vp] * 4 + [bp] + [i32] * 6 + [f32, i32] + [i64] * 4 + [vp, vp, vp]
+        L.gt_rotary_frequencies.restype = ctypes.c_int
+        L.gt_rotary_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, vp]
         _lib = L
     return _lib
 
@@ -506,3 +528,93 @@ def gt_feature_code_dweights(dtable, vectors, dweights) -> None:
     H, n_codes = dtable.shape
     _raise(lib().gt_feature_code_dweights(_ptr(dtable), _ptr(vectors), H, n_codes, _ptr(dweights), _stream()),
            "gt_feature_code_dweights")
+
+
+def _rows(t: Optional[torch.Tensor]):
+    """Address and row stride of a [T, heads, d] tensor whose rows are contiguous, but may lie apart (parts of a projection)."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise ValueError("expected a CUDA tensor [T, heads, d] with contiguous rows")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0
+
+
+def _same_dtype(dtype, *tensors) -> None:
+    for t in tensors:
+        if t is not None and t.dtype != dtype:
+            raise ValueError(f"expected tensors of type {dtype}")
+
+
+def gt_position_attn_fwd_workspace(batch: Batch, n_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    b = batch._c_pair()[1]
+    return int(lib().gt_position_attn_fwd_workspace(b, n_heads, n_kv_heads, head_dim))
+
+
+def _position_strides(q, k, v, dq=None, dk=None, dv=None):
+    """C struct of the row strides, and the addresses."""
+    got = [_rows(t) for t in (q, k, v, dq, dk, dv)]
+    return _GtRowStrides(*[s for _, s in got]), [p for p, _ in got]
+
+
+def gt_position_attn_fwd(q, k, v, slopes: Optional[torch.Tensor], prefix: Optional[torch.Tensor], batch: Batch,
+                         causal: bool, cap: float, out, lse, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention over token sequences: q [T, H, d], k and v [T, G, d] (rows may lie apart), slopes fp32 [H], prefix int32 [documents]."""
+    _, H, d = q.shape
+    G = k.shape[1]
+    _same_dtype(torch.bfloat16, q, k, v, out)
+    if workspace is None:
+        workspace = _workspace(gt_position_attn_fwd_workspace(batch, H, G, d), q.device)
+    strides, (pq, pk, pv, _, _, _) = _position_strides(q, k, v)
+    st = lib().gt_position_attn_fwd(pq, pk, pv, _ptr(slopes), _ptr(prefix), batch._c_pair()[1], H, G, d, ctypes.byref(strides),
+                                    int(causal), float(cap), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel(), _stream())
+    _raise(st, "gt_position_attn_fwd")
+    return workspace
+
+
+def gt_position_attn_bwd_workspace(batch: Batch, n_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    b = batch._c_pair()[1]
+    return int(lib().gt_position_attn_bwd_workspace(b, n_heads, n_kv_heads, head_dim))
+
+
+def gt_position_attn_bwd(q, k, v, out, dout, lse, slopes: Optional[torch.Tensor], prefix: Optional[torch.Tensor], batch: Batch,
+                         causal: bool, cap: float, dq, dk, dv, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradients of gt_position_attn_fwd; rows of q, k, v, dq, dk and dv may lie apart."""
+    _, H, d = q.shape
+    G = k.shape[1]
+    _same_dtype(torch.bfloat16, q, k, v, out, dout, dq, dk, dv)
+    if workspace is None:
+        workspace = _workspace(gt_position_attn_bwd_workspace(batch, H, G, d), q.device)
+    strides, (pq, pk, pv, pdq, pdk, pdv) = _position_strides(q, k, v, dq, dk, dv)
+    st = lib().gt_position_attn_bwd(pq, pk, pv, _ptr(out), _ptr(dout), _ptr(lse), _ptr(slopes), _ptr(prefix), batch._c_pair()[1],
+                                    H, G, d, ctypes.byref(strides), int(causal), float(cap), pdq, pdk, pdv,
+                                    _ptr(workspace), workspace.numel(), _stream())
+    _raise(st, "gt_position_attn_bwd")
+    return workspace
+
+
+def gt_rotary(q, k: Optional[torch.Tensor], frequencies, positions: Optional[torch.Tensor], batch: Batch, interleaved: bool,
+              scale: float, inverse: bool, q_out, k_out: Optional[torch.Tensor]) -> None:
+    """Rotary positions of q [T, H, d] and k [T, G, d] (or None) by frequencies fp64 [rot_dim / 2]; outputs may be the inputs."""
+    _, H, d = q.shape
+    _same_dtype(q.dtype, k, q_out, k_out)
+    _same_dtype(torch.float64, frequencies)
+    _same_dtype(torch.int32, positions)
+    if q.dtype not in DTYPES:
+        raise ValueError("expected bf16, fp16 or fp32")
+    if (k is None) != (k_out is None):
+        raise ValueError("expected k and k_out, or neither")
+    (pq, sq), (pk, sk), (oq, tq), (ok, tk) = (_rows(t) for t in (q, k, q_out, k_out))
+    st = lib().gt_rotary(pq, pk, _ptr(frequencies), _ptr(positions), batch._c_pair()[1], H, 0 if k is None else k.shape[1], d,
+                         2 * frequencies.numel(), DTYPES[q.dtype], int(interleaved), float(scale), int(inverse), sq, sk, tq, tk,
+                         oq, ok, _stream())
+    _raise(st, "gt_rotary")
+
+
+def gt_rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
+                          original_length: float = 0.0, low: float = 0.0, high: float = 0.0) -> torch.Tensor:
+    """The table for gt_rotary, fp64 [rot_dim / 2], on the CPU."""
+    out = torch.empty(max(int(rot_dim), 0) // 2, dtype=torch.float64)
+    st = lib().gt_rotary_frequencies(int(rot_dim), float(base), ROTARY_SCALINGS[scaling], float(factor), float(original_length),
+                                     float(low), float(high), out.data_ptr() or None)
+    _raise(st, "gt_rotary_frequencies")
+    return out

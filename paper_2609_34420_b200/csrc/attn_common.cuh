@@ -15,6 +15,8 @@ constexpr float kLn2 = 0.6931471805599453f;
 // (d x 1 x 128 elements), written to shared memory as 128 rows of 2d bytes with the
 // swizzle mode that matches the row length (128B for d=64, 64B for d=32, 32B for d=16).
 gt_status encode_thd_map(CUtensorMap* map, const void* base, int32_t n_total, int32_t n_heads, int32_t head_dim);
+// The same for rows that lie row_stride elements apart (a multiple of 8, n_heads * head_dim at least).
+gt_status encode_rows_map(CUtensorMap* map, const void* base, int32_t n_total, int32_t n_heads, int32_t head_dim, int64_t row_stride);
 
 // 2-D tensor map over the uint8 SPD matrix of a single graph (n rows of pitch round_up(n,16));
 // one box = box_rows rows x 128 key columns, written with the 128-byte swizzle (16-byte chunk c

@@ -1,0 +1,81 @@
+// What the forward and the backward of attention over token sequences share: which keys a query sees, the capped score, argument
+// checks.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "attn_common.cuh"
+#include "sm100_primitives.cuh"
+
+namespace gt {
+namespace position {
+
+// tanh(y) = y P(y^2) for |y| <= 1: the polynomial of degree 5 in y^2 whose largest relative error on that range is least (by the
+// exchange method of Remez), 5.9e-7.  A score x has |x| < cap nearly always, so that its tanh takes FMAs only and the special-function
+// unit is left to the exponentials; a warp that meets a larger score takes its tile again with tanh_any.  (tanh.approx.f32 is off by
+// 2^-11 relative: a score of 20 by 0.01, its probability by 1 %.)
+constexpr float kTanhReach = 1.0f;                 // of y^2
+constexpr float kTanh0 = 9.999994136e-01f, kTanh1 = -3.332904238e-01f, kTanh2 = 1.328143388e-01f, kTanh3 = -5.160567400e-02f,
+                kTanh4 = 1.674311506e-02f, kTanh5 = -3.067060327e-03f;
+
+template <bool B> struct Tag { static constexpr bool value = B; };
+
+__device__ __forceinline__ uint64_t both(float x) { return sm100::pack_f32x2(x, x); }
+
+// P(u) of two arguments u = y^2.
+__device__ __forceinline__ uint64_t tanh_ratio(uint64_t u)
+{
+    uint64_t r = sm100::fma_f32x2(both(kTanh5), u, both(kTanh4));
+    r = sm100::fma_f32x2(r, u, both(kTanh3));
+    r = sm100::fma_f32x2(r, u, both(kTanh2));
+    r = sm100::fma_f32x2(r, u, both(kTanh1));
+    return sm100::fma_f32x2(r, u, both(kTanh0));
+}
+// tanh(y) of any y: the polynomial within its reach, beyond it 1 - 2 / (1 + e^2y), which is off by 3e-7.
+__device__ __forceinline__ float tanh_any(float y)
+{
+    const float u = y * y;
+    float p = fmaf(kTanh5, u, kTanh4), r;
+    p = fmaf(p, u, kTanh3);
+    p = fmaf(p, u, kTanh2);
+    p = fmaf(p, u, kTanh1);
+    p = fmaf(p, u, kTanh0) * y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + sm100::ex2_approx(y * (2.0f * kLog2e))));
+    return u <= kTanhReach ? p : fmaf(-2.0f, r, 1.0f);
+}
+
+// A query at position i of a document of n tokens sees the document's keys [0, row_limit).
+__device__ __forceinline__ int32_t row_limit(bool causal, int32_t i, int32_t prefix, int32_t n) { return causal ? min(n, max(i + 1, prefix)) : n; }
+
+constexpr float kMaxCap = 1e6f;
+constexpr int64_t kMaxRowStride = (int64_t)1 << 38;
+
+inline gt_status validate(const gt_batch* batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, const int32_t* prefix, int32_t causal,
+                          float cap)
+{
+    const gt_status st = validate_batch(batch);
+    if (st != GT_OK) return st;
+    if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0) return GT_ERR_INVALID_ARG;
+    if (cap != 0.f && !(cap >= 1.f / kMaxCap && cap <= kMaxCap)) return GT_ERR_INVALID_ARG;
+    if (!causal && prefix != nullptr) return GT_ERR_INVALID_ARG;
+    if (head_dim != 32 && head_dim != 64) return GT_ERR_UNSUPPORTED;
+    if (n_heads > 65535 || batch->n_graphs > 65535) return GT_ERR_UNSUPPORTED;
+    return GT_OK;
+}
+
+// Elements from a row of a [T, heads, d] bf16 tensor to the next; 0: packed.  TMA copies and 16-byte accesses want whole 16 bytes.
+inline bool row_stride(int64_t given, int32_t heads, int32_t head_dim, int64_t* stride)
+{
+    *stride = given == 0 ? (int64_t)heads * head_dim : given;
+    return *stride >= (int64_t)heads * head_dim && *stride % 8 == 0 && *stride <= kMaxRowStride;
+}
+
+// Rows [first, 128) of a tile in shared memory are cleared by the calling warp, for MMAs that read the tile afterwards: what lies behind
+// a document's last row belongs to another one, and 0 x NaN is NaN.
+__device__ __forceinline__ void clear_rows(uint8_t* tile, int first, int row_bytes)
+{
+    for (int at = first * row_bytes + (int)(threadIdx.x & 31) * 16; at < 128 * row_bytes; at += 512) *(uint4*)(tile + at) = make_uint4(0u, 0u, 0u, 0u);
+}
+
+}  // namespace position
+}  // namespace gt

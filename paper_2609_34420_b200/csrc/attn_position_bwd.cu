@@ -1,0 +1,808 @@
+// gt_position_attn_bwd: gradient of attention over packed token sequences with respect to q, k and v (formulas: the header).
+//
+// One CTA owns one query head and one tile of 128 keys and walks over the query tiles that see any of them.  Scores are recomputed
+// TRANSPOSED (S^T = K Q^T, thread = key = TMEM lane), so that P^T and dS^T can go straight back to tensor memory as the A operands of
+// dV += P^T dO and dK += dS^T Q; dS^T is also written to shared memory (MN-major A operand) for dQ_i = dS K, which is added to an fp32
+// accumulator in global memory.  A mask is a range of queries for every key, so a thread compares column numbers with two bounds.
+//
+// The per-query terms are folded into the MMAs: a pre-pass writes for every (query, head) a row of 16 bf16 with -lse sqrt(d) and
+// -Delta, each split into three bf16 terms (24 mantissa bits); one extra K = 16 step against a constant tile of ones adds them.  With
+// capped scores the tanh comes between the product and lse, so that only Delta is folded and lse is read from shared memory.
+//
+// A query tile is two halves of 64 queries with a TMEM stage, MMAs and barriers of their own; while one half's MMAs run, the other
+// half's warps compute.  Three helper warps issue the MMAs; each accumulator and each part of a TMEM stage belongs to one of them, so
+// every reuse of tensor memory follows, in that thread's issue order, the MMA that reads the old contents.
+//
+//   warp 0        TMA producer: K, V once; Q_i, dO_i and the per-query rows through a 2-stage ring; clears what lies behind the document
+//   warps 1, 3, 2 MMA issuers: dV and the next S^T; dK and the next dP^T; dQ
+//   warps 4-19    softmax: warps 4-11 own queries [0,64) of every tile, warps 12-19 queries [64,128); within a half, four warps per 32
+//                 query columns
+//   warps 20-23   dQ reducer: TMEM -> shared memory -> TMA reduce-add into the fp32 accumulator
+//
+// TMEM columns, half g: S^T/P^T [128g, 128g+64)  dP^T/dS^T [128g+64, 128g+128);
+//               dV [256,320)  dK [320,384)  dQ [384,448)  K [448,480)  V [480,512) (bf16 pairs).
+#include <math.h>
+
+#include "attn_position.cuh"
+
+namespace gt {
+namespace {
+
+using namespace sm100;
+using namespace position;
+
+constexpr int kTile = 128;
+constexpr int kHalf = 64;                   // queries per TMEM stage
+constexpr int kStages = 2;
+constexpr int kThreads = 768;
+constexpr int kSoftmaxWarps = 16;
+constexpr int kExtCols = 16;                // bf16 per (query, head) row of folded terms
+constexpr int kExtTileBytes = kTile * kExtCols * 2;
+
+struct PositionBwdParams {
+    const int32_t* cu_seqlens;
+    const int32_t* prefix;
+    const float* slopes;
+    const float* lse;        // [H,T]
+    __nv_bfloat16* dk;
+    __nv_bfloat16* dv;
+    int64_t dk_row, dv_row;  // elements from a row to the next
+    float* dk_acc;           // [T,G,D] fp32 (workspace, zeroed) where heads share keys, else nullptr
+    float* dv_acc;
+    uint32_t* status;
+    const int4* list;        // packed batch: work list; block index = entry * heads + head (nullptr: grid of heads x tiles x documents)
+    int32_t n_total;
+    int32_t n_heads;
+    int32_t group;           // query heads per key head
+    int32_t causal;
+    int32_t early_release;   // let the next kernel start its set-up while this one runs
+    float c1;                // log2(e) / sqrt(d)
+    float scale;             // 1 / sqrt(d)
+    float to_tanh;           // 1 / (sqrt(d) cap)
+    float cap2;              // cap log2(e)
+};
+
+enum Barrier {
+    kBarKvFull = 0,
+    kBarQdoFull = 1,                         // [2]  Q_i, dO_i and the per-query rows of tile i
+    kBarStageEmpty = kBarQdoFull + kStages,  // [2]  commits behind the last MMAs that read Q_i / dO_i
+    kBarSFull = kBarStageEmpty + kStages,    // [2]  per half: S^T of the next tile is in tensor memory
+    kBarDpFull = kBarSFull + 2,              // [2]  per half: dP^T of the next tile
+    kBarPReady = kBarDpFull + 2,             // [2]  per half: 8 warp arrivals, P^T stored
+    kBarDsReady = kBarPReady + 2,            // [2]  per half: 8 warp arrivals, dS^T stored (tensor and shared memory)
+    kBarDqFull = kBarDsReady + 2,
+    kBarDqFree,
+    kBarKvTmem,                              //      8 warp arrivals: K and V rows copied to tensor memory
+    kBarKClear,                              //      K's rows behind the document are cleared
+    kBarQClear,                              //      ... and those of the last Q and dO tiles
+    kBarFinal,
+    kNumBarriers
+};
+constexpr int kNbDqStaged = 4, kNbDqStagingFree = 5;       // named barriers
+
+template <int D>
+struct Smem {
+    static constexpr int kRowBytes = D * 2;
+    static constexpr int kTileBytes = 128 * kRowBytes;
+    static constexpr int kK = 0;
+    static constexpr int kV = kK + kTileBytes;
+    static constexpr int kOnes = kV + kTileBytes;                   // two constant groups of 8 x 16 bf16 (256 B each)
+    static constexpr int kStageBytes = 2 * kTileBytes;              // Q_i then dO_i
+    static constexpr int kQ = kOnes + 1024;                         // [kStages] at stride kStageBytes
+    static constexpr int kDo = kQ + kTileBytes;                     // [kStages] at stride kStageBytes
+    static constexpr int kExt = kQ + kStages * kStageBytes;         // [kStages] per-query rows
+    static constexpr int kStg = kExt + kStages * kExtTileBytes;     // dQ staging: 128 rows x 32 floats
+    static constexpr int kDs = kStg + 16384;                        // dS^T: 2 atoms x 128 rows x 128 bytes
+    static constexpr int kLse = kDs + 32768;                        // [softmax warps][32] float
+    static constexpr int kBars = kLse + kSoftmaxWarps * 128;
+    static constexpr int kMisc = kBars + kNumBarriers * 8;
+    static constexpr int kDynamic = kMisc + 16 + 1024;              // slack for the 1024-byte alignment
+};
+
+// register budget: the CTA is launched with 768 x 80 registers; after the re-split it holds
+// 128 x 40 + 512 x 96 + 128 x 48 = 60416 <= 61440 (an increase can only draw on what the CTA owns)
+__device__ __forceinline__ void setmaxnreg_inc_96() { asm volatile("setmaxnreg.inc.sync.aligned.u32 96;"); }
+__device__ __forceinline__ void setmaxnreg_dec_48() { asm volatile("setmaxnreg.dec.sync.aligned.u32 48;"); }
+
+template <int D, bool kCap, bool kSlope>
+__global__ void __launch_bounds__(kThreads, 1)
+position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
+                    const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ CUtensorMap tmap_do,
+                    const __grid_constant__ CUtensorMap tmap_ext, const __grid_constant__ CUtensorMap tmap_dq,
+                    const PositionBwdParams p)
+{
+    using L = Smem<D>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    int h = blockIdx.x, g = blockIdx.z, kv_tile = blockIdx.y;
+    int32_t node0 = 0, n = p.n_total;
+    if (p.cu_seqlens) grid_wait();          // a single document's blocks set up their barriers and tensor memory before they wait
+    if (p.list) {
+        const int4 entry = p.list[blockIdx.x / (unsigned)p.n_heads];
+        if (entry.x < 0) return;
+        h = (int)(blockIdx.x % (unsigned)p.n_heads);
+        g = entry.x;
+        kv_tile = entry.y;
+        node0 = entry.z;
+        n = entry.w;
+    } else if (p.cu_seqlens) {
+        node0 = p.cu_seqlens[g];
+        n = p.cu_seqlens[g + 1] - node0;
+    }
+    const int32_t kv0 = kv_tile * kTile;
+    if (kv0 >= n) return;
+
+    uint64_t* bars = (uint64_t*)(smem + L::kBars);
+    uint32_t* misc = (uint32_t*)(smem + L::kMisc);
+    auto bar = [&](int i) { return smem_u32(&bars[i]); };
+    volatile uint32_t* abort_flag = &misc[1];
+    if (tid == 0) {
+        misc[1] = 0u;
+        mbar_init(bar(kBarKvFull), 1);
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(bar(kBarQdoFull + s), 1);
+            mbar_init(bar(kBarStageEmpty + s), 2);
+            mbar_init(bar(kBarSFull + s), 1);
+            mbar_init(bar(kBarDpFull + s), 1);
+            mbar_init(bar(kBarPReady + s), kSoftmaxWarps / 2);       // one arrival per warp
+            mbar_init(bar(kBarDsReady + s), kSoftmaxWarps / 2);
+        }
+        mbar_init(bar(kBarDqFull), 1);
+        mbar_init(bar(kBarDqFree), 4);
+        mbar_init(bar(kBarKvTmem), 8);
+        mbar_init(bar(kBarKClear), 1);
+        mbar_init(bar(kBarQClear), 1);
+        mbar_init(bar(kBarFinal), 3);
+        fence_mbar_init();
+    }
+    if (warp == 2) { tmem_alloc(smem_u32(&misc[0]), 512); tmem_relinquish(); }
+    if (!p.cu_seqlens) grid_wait();
+    const int32_t prefix = p.prefix ? p.prefix[g] : 0;
+    const int32_t q_lo = p.causal && kv0 >= prefix ? kv0 : 0;              // first query that sees a key of the tile, in whole tiles
+    const int32_t n_q = (n - q_lo + kTile - 1) / kTile;
+    const bool others_behind = node0 + n < p.n_total;
+    const bool k_ragged = others_behind && kv0 + kTile > n, q_ragged = others_behind && n % kTile != 0;
+    const int kv_head = h / p.group;
+    auto load_q_do = [&](int i) {
+        const int s = i & 1;
+        const int32_t row = node0 + q_lo + i * kTile;
+        mbar_arrive_expect_tx(bar(kBarQdoFull + s), 2 * L::kTileBytes + kExtTileBytes);
+        tma_load_3d(smem_u32(smem + L::kQ + s * L::kStageBytes), &tmap_q, bar(kBarQdoFull + s), 0, h, row);
+        tma_load_3d(smem_u32(smem + L::kDo + s * L::kStageBytes), &tmap_do, bar(kBarQdoFull + s), 0, h, row);
+        tma_load_3d(smem_u32(smem + L::kExt + s * kExtTileBytes), &tmap_ext, bar(kBarQdoFull + s), 0, h, row);
+    };
+    if (tid == 0) {                          // the first tiles are on their way while the block is still setting up
+        mbar_arrive_expect_tx(bar(kBarKvFull), 2 * L::kTileBytes);
+        tma_load_3d(smem_u32(smem + L::kK), &tmap_k, bar(kBarKvFull), 0, kv_head, node0 + kv0);
+        tma_load_3d(smem_u32(smem + L::kV), &tmap_v, bar(kBarKvFull), 0, kv_head, node0 + kv0);
+        load_q_do(0);
+    }
+    if (p.early_release) grid_release();
+    if (tid < 32) {
+        // 8 rows x 32 bytes per group in the 32-byte swizzle: the 16-byte half that holds columns 0..7 sits
+        // first in rows 0-3 and second in rows 4-7.  Group 0: ones in columns 0..2 (multiplies the -lse terms),
+        // group 1: ones in columns 8..10 (the -Delta terms).
+        const int grp_ = tid >> 4, row = (tid >> 1) & 7, phys_half = tid & 1;
+        const int logical_half = phys_half ^ (row >> 2);
+        const bool has_ones = logical_half == grp_;
+        *(uint4*)(smem + L::kOnes + tid * 16) = has_ones ? make_uint4(0x3f803f80u, 0x00003f80u, 0u, 0u) : make_uint4(0u, 0u, 0u, 0u);
+        fence_proxy_async_smem();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = misc[0];
+    constexpr uint32_t kColDv = 256, kColDk = 320, kColDq = 384, kColK = 448, kColV = 480;
+
+    if (warp < 4) {
+        setmaxnreg_dec_40();
+        if (warp == 0) {
+            // ------------------------------ TMA producer ------------------------------
+            if (k_ragged) {
+                mbar_wait(bar(kBarKvFull), 0, abort_flag, p.status, 309);
+                clear_rows(smem + L::kK, n - kv0, L::kRowBytes);
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(kBarKClear));
+            }
+            for (int i = 1; i < n_q; ++i) {
+                mbar_wait(bar(kBarStageEmpty + (i & 1)), ((i >> 1) & 1) ^ 1, abort_flag, p.status, 310);
+                if (lane == 0) load_q_do(i);
+                __syncwarp();
+            }
+            if (q_ragged) {                          // (the last tile's own phase: nothing is loaded behind it)
+                const int s = (n_q - 1) & 1, first = n - q_lo - (n_q - 1) * kTile;
+                mbar_wait(bar(kBarQdoFull + s), ((n_q - 1) >> 1) & 1, abort_flag, p.status, 311);
+                clear_rows(smem + L::kQ + s * L::kStageBytes, first, L::kRowBytes);
+                clear_rows(smem + L::kDo + s * L::kStageBytes, first, L::kRowBytes);
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(kBarQClear));
+            }
+        } else if (warp == 1 || warp == 3) {
+            // ------------------------------- MMA issuers -------------------------------
+            // warp 1: on "P^T(i) of a half stored": dV += P^T dO_i, then S^T of the next tile over the P^T just read
+            // warp 3: on "dS^T(i) of a half stored": dK += dS^T Q_i, then dP^T of the next tile over that dS^T
+            const bool on_p = warp == 1;
+            constexpr uint32_t idesc_in = make_idesc_bf16(128, kHalf, false, false);   // S^T, dP^T of 64 queries
+            constexpr uint32_t idesc_ts = make_idesc_bf16(128, D, false, true);        // A in TMEM, B MN-major
+            const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+            // constant A operand of the extra K step: every 8-row group reads the same 256 bytes (group stride 0)
+            const uint64_t desc_ones = make_smem_desc_stride(smem_u32(smem + L::kOnes + (on_p ? 0 : 256)), kExtCols * 2, 0, 0);
+            const int acc_b_off = on_p ? L::kDo : L::kQ;       // B of the accumulating MMA: dO_i (dV) / Q_i (dK)
+            const int in_b_off = on_p ? L::kQ : L::kDo;        // B of the next input MMA:   Q (S^T)  / dO (dP^T)
+            const uint32_t acc_col = on_p ? kColDv : kColDk;
+            const uint32_t reg_off = on_p ? 0 : kHalf;          // S^T/P^T or dP^T/dS^T part of a TMEM stage
+            const uint32_t in_a_col = on_p ? kColK : kColV;
+            const int bar_ready = on_p ? kBarPReady : kBarDsReady, bar_full = on_p ? kBarSFull : kBarDpFull;
+            auto issue_input = [&](int i, int sub) {            // (S^T - lse sqrt(d)) or (dP^T - Delta) of a half tile
+                const int s = i & 1;
+                const uint64_t db = make_smem_desc(smem_u32(smem + in_b_off + s * L::kStageBytes) + sub * kHalf * L::kRowBytes, L::kRowBytes, 0);
+                const uint64_t dext = make_smem_desc(smem_u32(smem + L::kExt + s * kExtTileBytes) + sub * kHalf * kExtCols * 2, kExtCols * 2, 0);
+                const uint32_t d = tm + sub * 128 + reg_off;
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks)             // A = K or V from tensor memory: 8 packed columns per K step
+                    mma_ts(d, tm + in_a_col + ks * 8, advance_desc(db, ks * 32), idesc_in, ks > 0);
+                if (!kCap || !on_p) mma_ss(d, desc_ones, dext, idesc_in, 1u);
+                mma_commit(bar(bar_full + sub));
+            };
+            auto wait_tile = [&](int i) {
+                mbar_wait(bar(kBarQdoFull + (i & 1)), (i >> 1) & 1, abort_flag, p.status, 321);
+                if (q_ragged && i == n_q - 1) mbar_wait(bar(kBarQClear), 0, abort_flag, p.status, 322);
+            };
+            mbar_wait(bar(kBarKvTmem), 0, abort_flag, p.status, 320);
+            wait_tile(0);
+            tc_fence_after();
+            if (elect_one()) { issue_input(0, 0); issue_input(0, 1); }
+            __syncwarp();
+            bool acc_started = false;           // the first MMA into the accumulator overwrites it
+            for (int i = 0; i < n_q; ++i) {
+                const int s = i & 1;
+                if (i + 1 < n_q) wait_tile(i + 1);
+#pragma unroll
+                for (int sub = 0; sub < 2; ++sub) {
+                    mbar_wait(bar(bar_ready + sub), i & 1, abort_flag, p.status, 323);
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t t_a = tm + sub * 128 + reg_off;
+                        const uint64_t db = make_smem_desc(smem_u32(smem + acc_b_off + s * L::kStageBytes) + sub * kHalf * L::kRowBytes, L::kRowBytes, 0);
+#pragma unroll
+                        for (int ks = 0; ks < kHalf / 16; ++ks)     // A: bf16 pairs of query group ks/2 at the start of its 32 columns
+                            mma_ts(tm + acc_col, t_a + (ks >> 1) * 32 + (ks & 1) * 8,
+                                   advance_desc(db, ks * 16 * L::kRowBytes), idesc_ts, (acc_started || ks > 0) ? 1u : 0u);
+                        if (sub == 1) {
+                            mma_commit(bar(kBarStageEmpty + s));    // this issuer's reads of Q_i / dO_i are done (the other one commits too)
+                            if (i + 1 == n_q) mma_commit(bar(kBarFinal));
+                        }
+                        if (i + 1 < n_q) issue_input(i + 1, sub);
+                    }
+                    __syncwarp();
+                    acc_started = true;
+                }
+            }
+        } else if (warp == 2) {
+            // ------------------------------- dQ issuer -------------------------------
+            constexpr uint32_t idesc_dq = make_idesc_bf16(128, D, true, true);         // A and B MN-major
+            const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+            const uint64_t desc_k = make_smem_desc(smem_u32(smem + L::kK), L::kRowBytes, 0);
+            const uint64_t da = make_smem_desc(smem_u32(smem + L::kDs), 128, 16384);
+            mbar_wait(bar(kBarKvFull), 0, abort_flag, p.status, 330);
+            if (k_ragged) mbar_wait(bar(kBarKClear), 0, abort_flag, p.status, 331);
+            for (int i = 0; i < n_q; ++i) {
+                // dQ_i = dS K once both halves have stored dS^T(i) and the reducer has drained dQ_{i-1}
+                mbar_wait(bar(kBarDsReady + 0), i & 1, abort_flag, p.status, 332);
+                mbar_wait(bar(kBarDsReady + 1), i & 1, abort_flag, p.status, 333);
+                mbar_wait(bar(kBarDqFree), (i & 1) ^ 1, abort_flag, p.status, 334);
+                tc_fence_after();
+                if (elect_one()) {
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks)
+                        mma_ss(tm + kColDq, advance_desc(da, ks * 2048), advance_desc(desc_k, ks * 16 * L::kRowBytes), idesc_dq, ks > 0);
+                    mma_commit(bar(kBarDqFull));
+                    if (i + 1 == n_q) mma_commit(bar(kBarFinal));
+                }
+                __syncwarp();
+            }
+        }
+    } else if (warp < 20) {
+        // ================================ softmax warps ================================
+        setmaxnreg_inc_96();
+        const int half = (warp - 4) >> 3;               // query half of every tile = TMEM stage
+        const int grp = (warp - 4) >> 2;                // query-column group: columns [32 grp, 32 grp + 32) of the tile
+        const int r = ((warp & 3) << 5) | lane;         // key row within the tile = TMEM lane
+        const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t tS = tmem + half * 128 + (grp & 1) * 32 + lane_off;
+        const uint32_t tDp = tS + kHalf;
+        const int32_t key = kv0 + r, key0 = kv0 + (warp & 3) * 32;               // this thread's key, the warp's first one
+        // queries [from, to) see the key
+        const int32_t from = p.causal && key >= prefix ? key : 0, to = key < n ? n : 0;
+        const int32_t last_from = p.causal && key0 + 31 >= prefix ? key0 + 31 : 0;               // largest `from` of the warp
+        const uint64_t c1c1 = both(p.c1);
+        [[maybe_unused]] const uint64_t to_tanh2 = both(p.to_tanh), cap22 = both(p.cap2);
+        [[maybe_unused]] const float slope2 = kSlope ? p.slopes[h] * kLog2e : 0.f;
+        [[maybe_unused]] float* s_lse = (float*)(smem + L::kLse) + (warp - 4) * 32;
+        // lse of the warp's queries, a lane each, fetched a tile ahead
+        [[maybe_unused]] auto fetch_lse = [&](int i) -> float {
+            const int32_t q = q_lo + i * kTile + grp * 32 + lane;
+            return q < n ? -kLog2e * p.lse[(size_t)h * p.n_total + node0 + q] : 0.f;
+        };
+        [[maybe_unused]] float next_lse = kCap ? fetch_lse(0) : 0.f;
+        uint8_t* ds_row = smem + L::kDs + half * 16384 + r * 128;
+
+        // K (warps 4-7) and V (warps 8-11) rows -> tensor memory, where they stay as the A operands of S^T = K Q^T and dP^T = V dO^T
+        if (warp < 12) {
+            mbar_wait(bar(kBarKvFull), 0, abort_flag, p.status, 344);
+            const uint8_t* src = smem + (warp < 8 ? L::kK : L::kV) + r * L::kRowBytes;
+            uint32_t w[D / 2];
+#pragma unroll
+            for (int c = 0; c < D / 8; ++c) {
+                const int phys = D == 64 ? (c ^ (r & 7)) : (c ^ ((r >> 1) & 3));     // 128-byte / 64-byte swizzle
+                const uint4 v4 = *(const uint4*)(src + (phys << 4));
+                w[4 * c] = v4.x; w[4 * c + 1] = v4.y; w[4 * c + 2] = v4.z; w[4 * c + 3] = v4.w;
+            }
+            const uint32_t dst = tmem + (warp < 8 ? kColK : kColV) + lane_off;
+            if constexpr (D == 64) tmem_st32(dst, w); else tmem_st16(dst, w);
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(kBarKvTmem));
+        }
+
+        for (int i = 0; i < n_q; ++i) {
+            const int32_t q0 = q_lo + i * kTile + grp * 32;                     // the group's first query
+            const bool masked = q0 < last_from || q0 + 32 > n || key0 + 32 > n;     // some pair of the warp's may not count
+            const int c_from = from - q0, c_to = to - q0;
+            // Penalty on distance: linear in the column where all queries lie behind the keys (or masked ones before them do not matter) or
+            // all before; else made for every element.
+            const bool behind = q0 >= key0 + 31 || (p.causal && key0 >= prefix), before = q0 + 31 <= key0;
+            [[maybe_unused]] const bool mixed = kSlope && !before && !behind;
+            [[maybe_unused]] const float step_slope = behind ? -slope2 : slope2;
+            if constexpr (kCap) {
+                __syncwarp();
+                s_lse[lane] = next_lse;
+                if (i + 1 < n_q) next_lse = fetch_lse(i + 1);
+                __syncwarp();
+            }
+            float pr[32];                            // P^T, then dS^T (capped scores: P^T (1 - tanh^2) in between)
+            uint32_t pk[16];
+            mbar_wait(bar(kBarSFull + half), i & 1, abort_flag, p.status, 340);
+            tc_fence_after();
+
+            // ---------------- P^T = exp2((S^T - lse sqrt(d)) c1), or exp2(cap log2(e) tanh(S^T / cap) - lse log2(e)) ----------------
+            float top_u = 0.f;
+            auto probabilities = [&](auto wide) {
+                uint32_t sv[32];
+                tmem_ld32(tS, sv);
+                tmem_wait_ld();
+#pragma unroll
+                for (int c = 0; c < 32; c += 2) {
+                    uint64_t add = both(0.f), x;
+                    if constexpr (kCap) {
+                        const float2 nl = *(const float2*)(s_lse + c);
+                        add = pack_f32x2(nl.x, nl.y);
+                    }
+                    if constexpr (kSlope) {
+                        if (mixed) add = add_f32x2(add, pack_f32x2(-slope2 * fabsf((float)(q0 + c - key)), -slope2 * fabsf((float)(q0 + c + 1 - key))));
+                        else add = fma_f32x2(both(step_slope), pack_f32x2((float)(q0 + c - key), (float)(q0 + c + 1 - key)), add);
+                    }
+                    const uint64_t raw = pack_u32x2(sv[c], sv[c + 1]);
+                    [[maybe_unused]] uint64_t t;
+                    if constexpr (kCap) {
+                        const uint64_t u = mul_f32x2(raw, to_tanh2);
+                        if constexpr (decltype(wide)::value) {
+                            float u0, u1;
+                            unpack_f32x2(u, u0, u1);
+                            t = pack_f32x2(tanh_any(u0), tanh_any(u1));
+                        } else {
+                            const uint64_t uu = mul_f32x2(u, u);
+                            float u0, u1;
+                            unpack_f32x2(uu, u0, u1);
+                            top_u = fmaxf(top_u, fmaxf(u0, u1));
+                            t = mul_f32x2(u, tanh_ratio(uu));
+                        }
+                        x = fma_f32x2(t, cap22, add);
+                    } else if constexpr (kSlope) {
+                        x = fma_f32x2(raw, c1c1, add);
+                    } else {
+                        x = mul_f32x2(raw, c1c1);
+                    }
+                    float lo, hi;
+                    unpack_f32x2(x, lo, hi);
+                    lo = ex2_approx(lo);
+                    hi = ex2_approx(hi);
+                    if (masked) {
+                        if (c < c_from || c >= c_to) lo = 0.f;
+                        if (c + 1 < c_from || c + 1 >= c_to) hi = 0.f;
+                    }
+                    pk[c >> 1] = pack_bf16x2(lo, hi);
+                    if constexpr (kCap) {
+                        const uint64_t minus = mul_f32x2(t, both(-1.f));
+                        unpack_f32x2(mul_f32x2(pack_f32x2(lo, hi), fma_f32x2(minus, t, both(1.f))), pr[c], pr[c + 1]);
+                    } else {
+                        pr[c] = lo;
+                        pr[c + 1] = hi;
+                    }
+                }
+            };
+            probabilities(Tag<false>{});
+            if constexpr (kCap)
+                if (__any_sync(0xffffffffu, !(top_u <= kTanhReach))) probabilities(Tag<true>{});
+            tmem_st16(tS, pk);                      // P^T of this group: 16 packed columns at the start of its range
+            uint32_t dpa[16], dpb[16];
+            mbar_wait(bar(kBarDpFull + half), i & 1, abort_flag, p.status, 341);
+            tc_fence_after();
+            tmem_ld16(tDp, dpa);
+            tmem_ld16(tDp + 16, dpb);
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(kBarPReady + half));    // dV of this half and the next S^T can go
+            tmem_wait_ld();
+
+            // ---------------- dS^T = P^T o (dP^T - Delta) ----------------
+            auto ds_round = [&](int rnd, const uint32_t (&dp)[16]) {
+#pragma unroll
+                for (int k = 0; k < 16; k += 2) {
+                    const int c = rnd * 16 + k;
+                    float lo, hi;
+                    unpack_f32x2(mul_f32x2(pack_f32x2(pr[c], pr[c + 1]), pack_u32x2(dp[k], dp[k + 1])), lo, hi);
+                    if (masked) {                    // (0 x NaN: a row of V that is another document's, or of this one's queries that do not see the key)
+                        if (c < c_from || c >= c_to) lo = 0.f;
+                        if (c + 1 < c_from || c + 1 >= c_to) hi = 0.f;
+                    }
+                    pk[c >> 1] = pack_bf16x2(lo, hi);
+                }
+            };
+            ds_round(0, dpa);
+            ds_round(1, dpb);
+            tmem_st16(tDp, pk);
+            // dQ of the previous tile has read the dS^T tile in shared memory
+            if (i > 0) mbar_wait(bar(kBarDqFull), (i - 1) & 1, abort_flag, p.status, 342);
+#pragma unroll
+            for (int c8 = 0; c8 < 4; ++c8)
+                *(uint4*)(ds_row + ((((grp & 1) * 4 + c8) ^ (r & 7)) << 4)) = make_uint4(pk[4 * c8], pk[4 * c8 + 1], pk[4 * c8 + 2], pk[4 * c8 + 3]);
+            tmem_wait_st();
+            fence_proxy_async_smem();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(kBarDsReady + half));
+        }
+
+        // ---------------- epilogue: dV (first half's warps) and dK (second half's) ----------------
+        mbar_wait(bar(kBarFinal), 0, abort_flag, p.status, 343);
+        tc_fence_after();
+        constexpr int kOC = D / 2;                  // output columns per thread
+        const int ch = grp & 1;
+        const uint32_t tacc = tmem + (half == 0 ? kColDv : kColDk) + ch * kOC + lane_off;
+        uint32_t o[kOC];
+        if constexpr (kOC == 32) tmem_ld32(tacc, o); else tmem_ld16(tacc, o);
+        tmem_wait_ld();
+        if (key < n) {
+            if (p.dk_acc != nullptr) {
+                const size_t at = ((size_t)(node0 + key) * (p.n_heads / p.group) + kv_head) * D + ch * kOC;
+                float4* dst = (float4*)((half == 0 ? p.dv_acc : p.dk_acc) + at);
+#pragma unroll
+                for (int k = 0; k < kOC / 4; ++k) red_add_f32x4(dst + k, o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+            } else {
+                const float mul = half == 0 ? 1.0f : p.scale;
+                __nv_bfloat16* row = half == 0 ? p.dv + (int64_t)(node0 + key) * p.dv_row : p.dk + (int64_t)(node0 + key) * p.dk_row;
+                uint4* dst = (uint4*)(row + h * D + ch * kOC);
+#pragma unroll
+                for (int k = 0; k < kOC / 8; ++k) {
+                    uint4 v;
+                    v.x = pack_bf16x2(__uint_as_float(o[8 * k]) * mul, __uint_as_float(o[8 * k + 1]) * mul);
+                    v.y = pack_bf16x2(__uint_as_float(o[8 * k + 2]) * mul, __uint_as_float(o[8 * k + 3]) * mul);
+                    v.z = pack_bf16x2(__uint_as_float(o[8 * k + 4]) * mul, __uint_as_float(o[8 * k + 5]) * mul);
+                    v.w = pack_bf16x2(__uint_as_float(o[8 * k + 6]) * mul, __uint_as_float(o[8 * k + 7]) * mul);
+                    dst[k] = v;
+                }
+            }
+        }
+    } else {
+        // ================================ dQ reducer ================================
+        // dQ_i (fp32, 128 x D) goes TMEM -> registers -> a staging buffer in 128-byte-swizzled rows of 32 floats, and from there to the
+        // fp32 accumulator with TMA reduce-add.  An SM's reduce engine moves about 19 bytes per clock, so it has to run all the time:
+        // with d = 64 two staging buffers alternate (the second one is the V tile, dead once V sits in tensor memory).
+        setmaxnreg_dec_48();
+        const int r = ((warp & 3) << 5) | lane;
+        const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+        constexpr int kStgBufs = D == 64 ? 2 : 1;
+        for (int i = 0; i < n_q; ++i) {
+            mbar_wait(bar(kBarDqFull), i & 1, abort_flag, p.status, 350);
+            tc_fence_after();
+            const bool own = q_lo + i * kTile + r < n;              // rows behind the document get zeros, whatever K holds
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+                uint8_t* stg = smem + (kStgBufs == 2 && c == 1 ? L::kV : L::kStg);
+                uint32_t o[32];
+                tmem_ld32(tmem + kColDq + c * 32 + lane_off, o);
+                tmem_wait_ld();
+                if (c == D / 32 - 1) { tc_fence_before(); __syncwarp(); if (lane == 0) mbar_arrive(bar(kBarDqFree)); }
+                if (warp == 20 && elect_one()) {        // the reduce that last used this buffer has read it
+                    if (kStgBufs == 2) bulk_wait_group_read1(); else bulk_wait_group_read0();
+                }
+                named_barrier_sync(kNbDqStagingFree, 128);
+                uint8_t* row = stg + r * 128;
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    *(uint4*)(row + ((k ^ (r & 7)) << 4)) = own ? make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]) : make_uint4(0u, 0u, 0u, 0u);
+                fence_proxy_async_smem();
+                named_barrier_sync(kNbDqStaged, 128);
+                if (warp == 20) {
+                    if (elect_one()) {
+                        tma_reduce_add_2d(&tmap_dq, smem_u32(stg), h * D + c * 32, node0 + q_lo + i * kTile);
+                        bulk_commit_group();
+                    }
+                    __syncwarp();
+                }
+            }
+        }
+        if (warp == 20 && elect_one()) bulk_wait_group0();      // all adds have landed before the CTA retires
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag) __nanosleep(200000);
+    if (warp == 2) tmem_dealloc(tmem, 512);
+}
+
+__device__ __forceinline__ void split3_bf16(float v, uint32_t& w01, uint32_t& w2)
+{
+    const __nv_bfloat16 hi = __float2bfloat16_rn(v);
+    const float r1 = v - __bfloat162float(hi);
+    const __nv_bfloat16 mid = __float2bfloat16_rn(r1);
+    const __nv_bfloat16 lo = __float2bfloat16_rn(r1 - __bfloat162float(mid));
+    w01 = (uint32_t)__bfloat16_as_ushort(hi) | ((uint32_t)__bfloat16_as_ushort(mid) << 16);
+    w2 = (uint32_t)__bfloat16_as_ushort(lo);
+}
+
+struct PrepareParams {
+    const __nv_bfloat16* out;
+    const __nv_bfloat16* dout;
+    const float* lse;
+    uint4* ext;
+    float4* acc;               // the fp32 accumulators, cleared
+    int4* list;                // packed batch: work list of the main kernel, made by the last blocks
+    const int32_t* cu_seqlens;
+    size_t n_acc;              // float4s of them
+    int32_t n_total, n_graphs, n_heads;
+    uint32_t row_blocks;       // thread blocks that work on rows
+    float sqrt_d;
+};
+
+// What the main kernel wants done before it, in one launch.  Row blocks: for every row (t, h), ext[t][h][0..2] = three-term bf16 split of
+// -lse sqrt(d), ext[t][h][8..10] = that of -Delta, Delta = sum_c dO[t,h,c] O[t,h,c], zeros elsewhere; and their share of the accumulators
+// is cleared.  A thread owns a row and adds its products in channel order (a row whose softmax has one key then has dP = Delta to the
+// bit); the rows reach it through shared memory, because 32 lanes that each walk along a row of their own ask the L1 for every line eight
+// times.  16-byte chunk c of row r lies at chunk c ^ (r & 7): eight neighbouring rows' chunks lie in different banks (D = 32: c ^ (r & 3)).
+constexpr int kPrepareThreads = 256, kPrepareRows = 128;
+template <int D>
+__global__ void __launch_bounds__(kPrepareThreads) position_prepare_kernel(const PrepareParams p)
+{
+    constexpr int kChunks = D / 8, kSwz = kChunks - 1;
+    __shared__ __align__(16) uint8_t s_do[kPrepareRows * 2 * D], s_o[kPrepareRows * 2 * D];
+    grid_wait();
+    grid_release();
+    if (blockIdx.x >= p.row_blocks) {
+        const int32_t w = (int32_t)((blockIdx.x - p.row_blocks) * (kPrepareThreads / 32) + (threadIdx.x >> 5));
+        if (w < p.n_graphs) write_work_list<kTile>(p.list, p.n_total / kTile + p.n_graphs, p.cu_seqlens, p.n_graphs, w);
+        return;
+    }
+    const size_t n_rows = (size_t)p.n_total * p.n_heads, row0 = (size_t)blockIdx.x * kPrepareRows;
+    const int rows = (int)(row0 + kPrepareRows < n_rows ? kPrepareRows : n_rows - row0);
+    const uint4* from_do = (const uint4*)p.dout + row0 * kChunks;
+    const uint4* from_o = (const uint4*)p.out + row0 * kChunks;
+    constexpr int kEach = kPrepareRows * kChunks / kPrepareThreads;
+    uint4 x[kEach], y[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int e = (int)threadIdx.x + i * kPrepareThreads;
+        if (e < rows * kChunks) { x[i] = from_do[e]; y[i] = from_o[e]; }
+    }
+    for (size_t i = (size_t)blockIdx.x * kPrepareThreads + threadIdx.x; i < p.n_acc; i += (size_t)p.row_blocks * kPrepareThreads)
+        p.acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int e = (int)threadIdx.x + i * kPrepareThreads, r = e / kChunks, c = e % kChunks;
+        if (e < rows * kChunks) {
+            *(uint4*)(s_do + r * 2 * D + ((c ^ (r & kSwz)) << 4)) = x[i];
+            *(uint4*)(s_o + r * 2 * D + ((c ^ (r & kSwz)) << 4)) = y[i];
+        }
+    }
+    __syncthreads();
+    const int r = (int)threadIdx.x;
+    if (r >= rows) return;
+    const size_t row = row0 + r;
+    float acc = 0.f;
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+        const uint4 b = *(const uint4*)(s_do + r * 2 * D + ((i ^ (r & kSwz)) << 4)), a = *(const uint4*)(s_o + r * 2 * D + ((i ^ (r & kSwz)) << 4));
+        const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            acc += __uint_as_float(aw[k] << 16) * __uint_as_float(bw[k] << 16);
+            acc += __uint_as_float(aw[k] & 0xffff0000u) * __uint_as_float(bw[k] & 0xffff0000u);
+        }
+    }
+    uint4 e0 = make_uint4(0u, 0u, 0u, 0u), e1 = make_uint4(0u, 0u, 0u, 0u);
+    // A row that is not finite, or belongs to no document, gets zero terms: it may share a 128-row tile with another document's rows.
+    const float l = p.lse[(row % p.n_heads) * p.n_total + row / p.n_heads];
+    if (isfinite(l) && isfinite(acc)) {
+        split3_bf16(-l * p.sqrt_d, e0.x, e0.y);
+        split3_bf16(-acc, e1.x, e1.y);
+    }
+    p.ext[2 * row] = e0;
+    p.ext[2 * row + 1] = e1;
+}
+
+struct FinishParams {
+    const float4* acc[3];      // dq, and with shared key heads dk, dv
+    __nv_bfloat16* to[3];
+    int64_t row[3];            // elements from a row to the next
+    float mul[3];
+    uint32_t vecs[3];          // groups of eight channels in a row, 0: nothing to do
+    const int32_t* cu_seqlens;
+    int32_t n_total, n_graphs;
+};
+
+// The fp32 sums, scaled and rounded once; eight channels a thread.
+__global__ void __launch_bounds__(256) position_finish_kernel(const FinishParams p)
+{
+    grid_wait();
+    grid_release();
+    const int32_t end = p.cu_seqlens ? p.cu_seqlens[p.n_graphs] : p.n_total;
+    const uint32_t all = p.vecs[0] + p.vecs[1] + p.vecs[2];
+    const uint64_t idx = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint64_t t = idx / all;
+    if (t >= (uint64_t)end) return;
+    uint32_t c = (uint32_t)(idx - t * all);
+    int of = 0;
+    if (c >= p.vecs[0]) { c -= p.vecs[0]; of = 1; }
+    if (of == 1 && c >= p.vecs[1]) { c -= p.vecs[1]; of = 2; }
+    const float4* src = p.acc[of] + 2 * (t * p.vecs[of] + c);
+    const float4 a = __ldcs(src), b = __ldcs(src + 1);
+    const float m = p.mul[of];
+    *(uint4*)(p.to[of] + (int64_t)t * p.row[of] + 8 * (int64_t)c) =
+        make_uint4(pack_bf16x2(a.x * m, a.y * m), pack_bf16x2(a.z * m, a.w * m), pack_bf16x2(b.x * m, b.y * m), pack_bf16x2(b.z * m, b.w * m));
+}
+
+struct Workspace {
+    size_t list_off, ext_off, acc_off, kv_bytes, total;
+};
+
+Workspace workspace_of(const gt_batch* b, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim)
+{
+    Workspace w{};
+    const size_t rows = (size_t)b->n_total * n_heads;
+    w.list_off = kHeaderBytes;
+    w.ext_off = w.list_off + list_bytes(b, kTile);
+    w.acc_off = w.ext_off + align_up(rows * kExtCols * 2, 256);
+    w.kv_bytes = n_heads > n_kv_heads ? (size_t)b->n_total * n_kv_heads * head_dim * sizeof(float) : 0;
+    w.total = w.acc_off + align_up(rows * head_dim * sizeof(float) + 2 * w.kv_bytes, 256);
+    return w;
+}
+
+template <int D, bool kCap, bool kSlope>
+gt_status launch(const CUtensorMap (&maps)[6], PositionBwdParams p, const gt_batch* batch, cudaStream_t s)
+{
+    auto kern = position_bwd_kernel<D, kCap, kSlope>;
+    static std::atomic<uint64_t> granted{0};
+    const gt_status st = grant_smem(kern, granted, Smem<D>::kDynamic);
+    if (st != GT_OK) return st;
+    const dim3 grid = p.list ? dim3((unsigned)(list_entries(batch, kTile) * p.n_heads))
+                             : dim3((unsigned)p.n_heads, (unsigned)((batch->max_seqlen + kTile - 1) / kTile), (unsigned)batch->n_graphs);
+    // With several waves of blocks the early start of the next kernel slows the dispatch of this one's.
+    p.early_release = (int64_t)grid.x * grid.y * grid.z <= sm_count();
+    return launch_overlapped(kern, grid, kThreads, Smem<D>::kDynamic, s, maps[0], maps[1], maps[2], maps[3], maps[4], maps[5], p);
+}
+
+}  // namespace
+}  // namespace gt
+
+extern "C" size_t gt_position_attn_bwd_workspace(const gt_batch* batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim)
+{
+    if (gt::position::validate(batch, n_heads, n_kv_heads, head_dim, nullptr, 0, 0.f) != GT_OK) return 0;
+    return gt::workspace_of(batch, n_heads, n_kv_heads, head_dim).total;
+}
+
+extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const void* v, const void* out, const void* dout, const float* lse,
+                                          const float* slopes, const int32_t* prefix,
+                                          const gt_batch* batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                          const gt_row_strides* strides, int32_t causal, float cap,
+                                          void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes, void* stream)
+{
+    using namespace gt;
+    gt_status st = position::validate(batch, n_heads, n_kv_heads, head_dim, prefix, causal, cap);
+    if (st != GT_OK) return st;
+    if (!q || !k || !v || !out || !dout || !lse || !dq || !dk || !dv) return GT_ERR_INVALID_ARG;
+    if (misaligned16(q) || misaligned16(k) || misaligned16(v) || misaligned16(out) || misaligned16(dout) || misaligned16(dq) || misaligned16(dk) ||
+        misaligned16(dv))
+        return GT_ERR_INVALID_ARG;
+    const gt_row_strides given = strides ? *strides : gt_row_strides{};
+    const int64_t in[6] = {given.q, given.k, given.v, given.dq, given.dk, given.dv};
+    int64_t row[6];
+    for (int i = 0; i < 6; ++i)
+        if (!position::row_stride(in[i], i % 3 == 0 ? n_heads : n_kv_heads, head_dim, &row[i])) return GT_ERR_INVALID_ARG;
+    const Workspace w = workspace_of(batch, n_heads, n_kv_heads, head_dim);
+    if (workspace == nullptr || misaligned16(workspace) || workspace_bytes < w.total) return GT_ERR_WORKSPACE;
+    if (sm_count() <= 0) return GT_ERR_NO_DEVICE;
+    uint8_t* ws = (uint8_t*)workspace;
+    const int32_t T = batch->n_total;
+    float* dq_acc = (float*)(ws + w.acc_off);
+    CUtensorMap maps[6];
+    if ((st = encode_rows_map(&maps[0], q, T, n_heads, head_dim, row[0])) != GT_OK) return st;
+    if ((st = encode_rows_map(&maps[1], k, T, n_kv_heads, head_dim, row[1])) != GT_OK) return st;
+    if ((st = encode_rows_map(&maps[2], v, T, n_kv_heads, head_dim, row[2])) != GT_OK) return st;
+    if ((st = encode_thd_map(&maps[3], dout, T, n_heads, head_dim)) != GT_OK) return st;
+    if ((st = encode_thd_map(&maps[4], ws + w.ext_off, T, n_heads, kExtCols)) != GT_OK) return st;
+    if ((st = encode_dq_map(&maps[5], dq_acc, T, n_heads, head_dim)) != GT_OK) return st;
+    PositionBwdParams p{};
+    p.cu_seqlens = batch->cu_seqlens;
+    p.prefix = prefix;
+    p.slopes = slopes;
+    p.lse = lse;
+    p.dk = (__nv_bfloat16*)dk;
+    p.dv = (__nv_bfloat16*)dv;
+    p.dk_row = row[4];
+    p.dv_row = row[5];
+    if (w.kv_bytes > 0) {
+        p.dk_acc = dq_acc + (size_t)T * n_heads * head_dim;
+        p.dv_acc = p.dk_acc + (size_t)T * n_kv_heads * head_dim;
+    }
+    p.status = (uint32_t*)workspace;
+    if (batch->n_graphs > 1 && list_saves(batch, kTile, n_heads, 0)) p.list = (const int4*)(ws + w.list_off);
+    p.n_total = T;
+    p.n_heads = n_heads;
+    p.group = n_heads / n_kv_heads;
+    p.causal = causal != 0;
+    p.scale = 1.0f / sqrtf((float)head_dim);
+    p.c1 = kLog2e * p.scale;
+    p.to_tanh = cap > 0.f ? p.scale / cap : 0.f;
+    p.cap2 = cap * kLog2e;
+    cudaStream_t s = (cudaStream_t)stream;
+
+    PrepareParams pre{};
+    pre.out = (const __nv_bfloat16*)out;
+    pre.dout = (const __nv_bfloat16*)dout;
+    pre.lse = lse;
+    pre.ext = (uint4*)(ws + w.ext_off);
+    pre.acc = (float4*)dq_acc;
+    pre.list = const_cast<int4*>(p.list);
+    pre.cu_seqlens = batch->cu_seqlens;
+    pre.n_acc = ((size_t)T * n_heads * head_dim * sizeof(float) + 2 * w.kv_bytes) / 16;
+    pre.n_total = T;
+    pre.n_graphs = batch->n_graphs;
+    pre.n_heads = n_heads;
+    pre.row_blocks = (uint32_t)(((size_t)T * n_heads + kPrepareRows - 1) / kPrepareRows);
+    pre.sqrt_d = sqrtf((float)head_dim);
+    const uint32_t list_blocks = p.list ? (uint32_t)((batch->n_graphs + kPrepareThreads / 32 - 1) / (kPrepareThreads / 32)) : 0;
+    auto prepare = head_dim == 64 ? position_prepare_kernel<64> : position_prepare_kernel<32>;
+    if ((st = launch_overlapped(prepare, dim3(pre.row_blocks + list_blocks), kPrepareThreads, 0, s, pre)) != GT_OK) return st;
+
+    auto go = [&](auto d, auto capped) {
+        constexpr int D = decltype(d)::value ? 64 : 32;
+        return slopes ? launch<D, decltype(capped)::value, true>(maps, p, batch, s) : launch<D, decltype(capped)::value, false>(maps, p, batch, s);
+    };
+    if (head_dim == 64) st = cap > 0.f ? go(Tag<true>{}, Tag<true>{}) : go(Tag<true>{}, Tag<false>{});
+    else st = cap > 0.f ? go(Tag<false>{}, Tag<true>{}) : go(Tag<false>{}, Tag<false>{});
+    if (st != GT_OK) return st;
+
+    FinishParams f{};
+    const float* acc[3] = {dq_acc, p.dk_acc, p.dv_acc};
+    void* const to[3] = {dq, dk, dv};
+    for (int i = 0; i < 3; ++i) {
+        f.acc[i] = (const float4*)acc[i];
+        f.to[i] = (__nv_bfloat16*)to[i];
+        f.row[i] = row[3 + i];
+        f.mul[i] = i < 2 ? p.scale : 1.0f;
+        f.vecs[i] = acc[i] ? (uint32_t)((i == 0 ? n_heads : n_kv_heads) * head_dim / 8) : 0u;
+    }
+    f.cu_seqlens = batch->cu_seqlens;
+    f.n_total = T;
+    f.n_graphs = batch->n_graphs;
+    const uint64_t threads = (uint64_t)T * (f.vecs[0] + f.vecs[1] + f.vecs[2]);
+    if ((threads + 255) / 256 > 0x7fffffffull) return GT_ERR_UNSUPPORTED;
+    return launch_overlapped(position_finish_kernel, dim3((unsigned)((threads + 255) / 256)), 256, 0, s, f);
+}

@@ -1,0 +1,552 @@
+// gt_position_attn_fwd: attention over packed token sequences,
+//     out_i = sum_j softmax_j(S_i)_j v_j,   S_ij = cap tanh(q_i . k_j / (sqrt(d) cap)) - slopes[h] |i - j|,
+// over the keys that the document, the causal order and the prefix leave a query.  Positions are indices, so nothing but q, k and v is read.
+//
+// One CTA = one head x 256 query rows (two 128-row tiles, so that the tensor pipe works on one while the other is in its softmax) x the
+// key tiles that any of its rows sees.
+//
+//   warp 0      TMA producer: Q once; K and V through 2-stage rings
+//   warp 1      issues S_t = Q_t K^T for both query tiles
+//   warp 3      issues O_t += P_t V (A from TMEM, B = V as MN-major); clears what lies behind the document in its last V tile
+//   warps 4-19  softmax: 8 warps per query tile, 4 per half of the 128 key columns (thread = query row = TMEM lane, 64 scores)
+//
+// The key tiles come from the diagonal down to the document's beginning, then the ones behind the diagonal: with a penalty on distance
+// the scores fall along that way, so that a row's reference stays in reach.  A causal block of two tiles begins with a key tile that
+// only the second one sees; the first one skips that step.
+//
+// Softmax: a tile is exponentiated against the row's reference at once (0 at first), without a look at its maximum; the tile's row sum
+// tells whether the reference was out of reach, and only then it is redone with the maximum first.  References are whole numbers in log2
+// units, so rescale factors are exact.  The capped score's polynomial is tried and redone in the same way.
+//
+// TMEM columns: three score buffers [0,128) [128,256) [256,384), used in turn by the steps (key tile, query tile), so that the S MMA of
+// a step never waits for a softmax; P overwrites the part of a buffer that its own thread has read; O_0 [384,448), O_1 [448,512).
+#include <math.h>
+
+#include "attn_position.cuh"
+
+namespace gt {
+namespace {
+
+using namespace sm100;
+using namespace position;
+
+constexpr int kTile = 128;                    // rows of a query tile, keys of a key tile
+constexpr int kStages = 2;                    // of the K ring and of the V ring
+constexpr int kCols = 64;                     // score columns of a softmax thread
+constexpr int kCW = 16;                       // columns per TMEM load
+constexpr float kSumThreshold = 0x1p24f;       // tile row sum above which the reference is raised
+constexpr float kPeekReach = 24.0f;            // log2 units within which a row's first scores leave the starting reference as it is
+
+struct PositionFwdParams {
+    const int32_t* cu_seqlens;
+    const int32_t* prefix;
+    const float* slopes;
+    __nv_bfloat16* out;        // [T,H,D]
+    float* lse;                // [H,T]
+    uint32_t* status;
+    const int4* list;          // packed batch: work list; block index = entry * heads + head (nullptr: grid of heads x blocks x documents)
+    int32_t n_total;
+    int32_t n_heads;
+    int32_t group;             // query heads per key head
+    int32_t causal;
+    int32_t early_release;     // let the next kernel start its set-up while this one runs
+    float c1;                  // log2(e) / sqrt(d)
+    float to_tanh;             // 1 / (sqrt(d) cap)
+    float cap2;                // cap log2(e)
+};
+
+enum Barrier {
+    kBarQFull = 0,
+    kBarKFull = 1,                        // [kStages]
+    kBarKEmpty = kBarKFull + kStages,     // [kStages]  commit behind the S MMAs of the key tile
+    kBarVFull = kBarKEmpty + kStages,     // [kStages]
+    kBarVEmpty = kBarVFull + kStages,     // [kStages]  commit behind the PV MMAs of the key tile
+    kBarSFull = kBarVEmpty + kStages,     // [3]  per score buffer
+    kBarBufFree = kBarSFull + 3,          // [3]  P of the buffer consumed by its PV MMA
+    kBarPFull = kBarBufFree + 3,          // [2 tiles][2 parities of the tile's steps]
+    kBarODone = kBarPFull + 4,            // [2 tiles][2 parities]
+    kNumBarriers = kBarODone + 4
+};
+
+template <int D>
+struct Smem {
+    static constexpr int kRowBytes = D * 2;
+    static constexpr int kTileBytes = 128 * kRowBytes;
+    static constexpr int kQ = 0;
+    static constexpr int kK = kQ + 2 * kTileBytes;
+    static constexpr int kV = kK + kStages * kTileBytes;
+    static constexpr int kXchg = kV + kStages * kTileBytes;      // [2 tiles][max | sum][2 halves][128 rows] float
+    static constexpr int kBars = kXchg + 2 * 512 * 4;
+    static constexpr int kMisc = kBars + kNumBarriers * 8;
+    static constexpr int kDynamic = kMisc + 16 + 1024;           // slack for the 1024-byte alignment
+};
+
+constexpr int kNbPair = 2;                    // named barriers: + 4 t + lane quarter, the two warps that share 32 query rows
+
+// kTiles = 1: blocks of one query tile, for grids that would leave half of the SMs idle or more.
+template <int D, bool kCap, bool kSlope, int kTiles>
+__global__ void __launch_bounds__(128 + 256 * kTiles, 1)
+position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
+                    const __grid_constant__ CUtensorMap tmap_v, const PositionFwdParams p)
+{
+    using L = Smem<D>;
+    constexpr int kRows = kTile * kTiles, kBuffers = kTiles + 1;
+    constexpr uint32_t kOCol = 384;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    int h = blockIdx.x, g = blockIdx.z;
+    if (p.cu_seqlens) grid_wait();          // a single document's blocks set up their barriers and tensor memory before they wait
+    int32_t node0 = 0, n = p.n_total, q_block = blockIdx.y;
+    if (p.list) {
+        const int4 entry = p.list[blockIdx.x / (unsigned)p.n_heads];
+        if (entry.x < 0) return;
+        h = (int)(blockIdx.x % (unsigned)p.n_heads);
+        g = entry.x;
+        q_block = entry.y;
+        node0 = entry.z;
+        n = entry.w;
+    } else if (p.cu_seqlens) {
+        node0 = p.cu_seqlens[g];
+        n = p.cu_seqlens[g + 1] - node0;
+    }
+    if (q_block * kRows >= n) return;
+    if (p.causal) q_block = (n - 1) / kRows - q_block;               // the blocks with the most keys first
+    const int32_t q0 = q_block * kRows, n_tiles = (n + kTile - 1) / kTile;
+    uint64_t* bars = (uint64_t*)(smem + L::kBars);
+    uint32_t* misc = (uint32_t*)(smem + L::kMisc);       // [0] TMEM base, [1] abort flag
+    auto bar = [&](int i) { return smem_u32(&bars[i]); };
+    volatile uint32_t* abort_flag = &misc[1];
+    if (tid == 0) {
+        misc[1] = 0u;
+        mbar_init(bar(kBarQFull), 1);
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(bar(kBarKFull + s), 1);
+            mbar_init(bar(kBarKEmpty + s), 1);
+            mbar_init(bar(kBarVFull + s), 1);
+            mbar_init(bar(kBarVEmpty + s), 1);
+        }
+        for (int b = 0; b < 3; ++b) { mbar_init(bar(kBarSFull + b), 1); mbar_init(bar(kBarBufFree + b), 1); }
+        for (int t = 0; t < 4; ++t) { mbar_init(bar(kBarPFull + t), 8); mbar_init(bar(kBarODone + t), 1); }       // (P: one arrival per warp)
+        fence_mbar_init();
+    }
+    if (warp == 1) { tmem_alloc(smem_u32(&misc[0]), 512); tmem_relinquish(); }
+    if (!p.cu_seqlens) grid_wait();
+    const int32_t prefix = p.prefix ? min(n, p.prefix[g]) : 0;
+    const int32_t diagonal = min(q_block * kTiles + kTiles - 1, n_tiles - 1);
+    const int32_t n_kv = p.causal ? max(diagonal + 1, (prefix + kTile - 1) / kTile) : n_tiles;
+    // key tiles that the first query tile does not see: the block's first one, or none
+    const int skip = kTiles == 2 && p.causal && diagonal * kTile >= q0 + kTile && prefix <= diagonal * kTile ? 1 : 0;
+    auto tile_of = [&](int s) { return s <= diagonal ? diagonal - s : s; };
+    // the document's last V tile, if rows of another one follow in it
+    const int32_t ragged_tile = n % kTile != 0 && node0 + n < p.n_total ? n_tiles - 1 : -1;
+    const int kv_head = h / p.group;
+    auto load_k = [&](int s) {
+        const int st = s % kStages;
+        mbar_arrive_expect_tx(bar(kBarKFull + st), L::kTileBytes);
+        tma_load_3d(smem_u32(smem + L::kK + st * L::kTileBytes), &tmap_k, bar(kBarKFull + st), 0, kv_head, node0 + tile_of(s) * kTile);
+    };
+    auto load_v = [&](int s) {
+        const int st = s % kStages;
+        mbar_arrive_expect_tx(bar(kBarVFull + st), L::kTileBytes);
+        tma_load_3d(smem_u32(smem + L::kV + st * L::kTileBytes), &tmap_v, bar(kBarVFull + st), 0, kv_head, node0 + tile_of(s) * kTile);
+    };
+    if (tid == 0) {                          // the first tiles are on their way while the block is still setting up
+        mbar_arrive_expect_tx(bar(kBarQFull), kTiles * L::kTileBytes);
+        for (int t = 0; t < kTiles; ++t)
+            tma_load_3d(smem_u32(smem + L::kQ + t * L::kTileBytes), &tmap_q, bar(kBarQFull), 0, h, node0 + q0 + t * kTile);
+        load_k(0);
+        load_v(0);
+    }
+    if (p.early_release) grid_release();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = misc[0];
+
+    if (warp < 4) {
+        if constexpr (kTiles == 2) setmaxnreg_dec_32();
+        if (warp == 0) {
+            for (int s = 1; s < n_kv; ++s) {
+                mbar_wait(bar(kBarKEmpty + s % kStages), ((s / kStages) & 1) ^ 1, abort_flag, p.status, 210);
+                if (lane == 0) load_k(s);
+                mbar_wait(bar(kBarVEmpty + s % kStages), ((s / kStages) & 1) ^ 1, abort_flag, p.status, 211);
+                if (lane == 0) load_v(s);
+                __syncwarp();
+            }
+        } else if (warp == 1) {
+            constexpr uint32_t idesc_s = make_idesc_bf16(128, 128, false, false);
+            const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+            const uint64_t desc_q0 = make_smem_desc(smem_u32(smem + L::kQ), L::kRowBytes, 0);
+            const uint64_t desc_k0 = make_smem_desc(smem_u32(smem + L::kK), L::kRowBytes, 0);
+            mbar_wait(bar(kBarQFull), 0, abort_flag, p.status, 220);
+            for (int s = 0; s < n_kv; ++s) {
+                const int ks = s % kStages;
+                mbar_wait(bar(kBarKFull + ks), (s / kStages) & 1, abort_flag, p.status, 221);
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    if (kTiles == 2 && t == 0 && s < skip) continue;
+                    const int step = kTiles * s + t - skip, b = step % kBuffers;
+                    if (step >= kBuffers) mbar_wait(bar(kBarBufFree + b), (step / kBuffers - 1) & 1, abort_flag, p.status, 222);
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint64_t da = advance_desc(desc_q0, t * L::kTileBytes), db = advance_desc(desc_k0, ks * L::kTileBytes);
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k)
+                            mma_ss(tm + b * 128, advance_desc(da, k * 32), advance_desc(db, k * 32), idesc_s, k > 0);
+                        mma_commit(bar(kBarSFull + b));
+                        if (t == kTiles - 1) mma_commit(bar(kBarKEmpty + ks));
+                    }
+                    __syncwarp();
+                }
+            }
+        } else if (warp == 3) {
+            constexpr uint32_t idesc_o = make_idesc_bf16(128, D, false, true);
+            const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+            const uint64_t desc_v0 = make_smem_desc(smem_u32(smem + L::kV), L::kRowBytes, 0);
+            for (int s = 0; s < n_kv; ++s) {
+                const int vs = s % kStages;
+                mbar_wait(bar(kBarVFull + vs), (s / kStages) & 1, abort_flag, p.status, 230);
+                if (tile_of(s) == ragged_tile) {
+                    clear_rows(smem + L::kV + vs * L::kTileBytes, n - ragged_tile * kTile, L::kRowBytes);
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                }
+                const uint64_t dv = advance_desc(desc_v0, vs * L::kTileBytes);
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    if (kTiles == 2 && t == 0 && s < skip) continue;
+                    const int b = (kTiles * s + t - skip) % kBuffers, own = t == 0 ? s - skip : s;       // own: the query tile's steps so far
+                    mbar_wait(bar(kBarPFull + 2 * t + (own & 1)), (own >> 1) & 1, abort_flag, p.status, 232);
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < kTile / 16; ++k)      // P of key half hf sits at the start of that half's score columns
+                            mma_ts(tm + kOCol + t * 64, tm + b * 128 + (k / 4) * kCols + (k % 4) * 8, advance_desc(dv, k * 16 * L::kRowBytes), idesc_o,
+                                   own > 0 || k > 0 ? 1u : 0u);
+                        mma_commit(bar(kBarODone + 2 * t + (own & 1)));
+                        mma_commit(bar(kBarBufFree + b));
+                        if (t == kTiles - 1) mma_commit(bar(kBarVEmpty + vs));
+                    }
+                    __syncwarp();
+                }
+            }
+        }
+    } else {
+        // =================================== softmax warps ===================================
+        if constexpr (kTiles == 2) setmaxnreg_inc_112();
+        const int sw = warp - 4;
+        const int t = sw >> 3, hf = (sw >> 2) & 1;
+        const int r = ((warp & 3) << 5) | lane;
+        const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+        constexpr int kOC = D / 2;                       // output columns per thread
+        const uint32_t tO = tmem + kOCol + t * 64 + hf * kOC + lane_off;
+        const uint32_t pair_bar = kNbPair + t * 4 + (warp & 3);
+        float* xchg = (float*)(smem + L::kXchg) + t * 512;
+        const int32_t q = q0 + t * kTile + r;                                   // this thread's query
+        const int32_t limit = row_limit(p.causal, q, prefix, n);
+        const int32_t least_limit = row_limit(p.causal, q0 + t * kTile + (warp & 3) * 32, prefix, n);        // of the warp's rows
+        const int32_t first = t == 0 ? skip : 0;
+        float m = 0.f, l = 0.f;
+        bool wide = false;                               // kCap: a score was out of the polynomial's reach
+        const uint64_t c1c1 = both(p.c1);
+        [[maybe_unused]] const uint64_t to_tanh2 = both(p.to_tanh);
+        [[maybe_unused]] const float slope2 = kSlope ? p.slopes[h] * kLog2e : 0.f;
+
+        uint32_t sa[kCW], sb[kCW];              // score chunks, alternating
+        uint32_t tS = 0;                        // this thread's score columns of the current step
+        auto load_chunk = [&](int c, uint32_t (&sr)[kCW]) { tmem_ld16(tS + c * kCW, sr); };
+        // first chunk of a step's scores: fetched at the end of the step before, behind the P store
+        auto begin_step = [&](int s) {
+            const int step = kTiles * s + t - skip, b = step % kBuffers;
+            tS = tmem + b * 128 + hf * kCols + lane_off;
+            mbar_wait(bar(kBarSFull + b), (step / kBuffers) & 1, abort_flag, p.status, 250);
+            tc_fence_after();
+            load_chunk(0, sa);
+        };
+        begin_step(first);
+
+        for (int s = first; s < n_kv; ++s) {
+            const int own = s - first;
+            const int32_t kv0 = tile_of(s) * kTile + hf * kCols;       // this thread's first key
+            const bool ragged = kv0 + kCols > least_limit;             // some row of the warp does not see all of the columns
+            const int valid = limit - kv0;                             // columns that this thread's row sees (may be <= 0)
+            // Penalty on distance.  Where no key lies behind the query (or, for masked ones, it does not matter) it is linear in the
+            // column: (key - query) slope.  Otherwise keys behind all of the warp's rows have it the other way round, and in between
+            // a distance is made for every element.
+            const int32_t row0 = q0 + t * kTile + (warp & 3) * 32;
+            const bool before = kv0 + kCols - 1 <= row0 || (p.causal && kv0 >= prefix), behind = kv0 >= row0 + 31;
+            [[maybe_unused]] const bool mixed = kSlope && !before && !behind;
+            [[maybe_unused]] const float step_slope = before ? slope2 : -slope2;
+            uint32_t pk[32];                       // P of this thread's columns, bf16 pairs
+            float tile_sum = 0.f;
+            bool loaded = true;                    // chunk 0 is already on its way
+            bool exact = false;                    // take the tile maximum first
+
+            // Is the starting reference in reach of the first tile?  Four of the thread's first 16 scores tell.
+            if (own == 0) {
+                tmem_wait_ld();
+                float top = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float x = __uint_as_float(sa[4 * i]) * p.c1;
+                    if constexpr (kCap) x = fminf(fmaxf(x, -p.cap2), p.cap2);
+                    if constexpr (kSlope) x -= slope2 * fabsf((float)(kv0 + 4 * i - q));
+                    if (4 * i < valid) top = fmaxf(top, x);
+                }
+                exact = named_barrier_or(pair_bar, 64, valid > 0 && !(fabsf(top) <= kPeekReach));   // (a half without valid columns has no say)
+            }
+
+            // Scores of eight consecutive columns in log2 units, plus `add`; `far`: beyond the polynomial's reach.
+            float top_u = 0.f;
+            auto scores8 = [&](const uint32_t* sr, int col, float add, auto far, float (&x)[8]) {
+                uint64_t base = both(add);
+                if constexpr (kSlope)
+                    if (!mixed) base = both(fmaf(step_slope, (float)(kv0 + col - q), add));
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) {
+                    const uint64_t raw = pack_u32x2(sr[i], sr[i + 1]);
+                    uint64_t a = base, y;
+                    if constexpr (kSlope)
+                        if (!mixed) a = add_f32x2(base, pack_f32x2(step_slope * (float)i, step_slope * (float)(i + 1)));
+                    if constexpr (kCap && decltype(far)::value) {
+                        float u0, u1, a0, a1;
+                        unpack_f32x2(mul_f32x2(raw, to_tanh2), u0, u1);
+                        unpack_f32x2(a, a0, a1);
+                        y = pack_f32x2(fmaf(p.cap2, tanh_any(u0), a0), fmaf(p.cap2, tanh_any(u1), a1));
+                    } else if constexpr (kCap) {
+                        const uint64_t u = mul_f32x2(raw, to_tanh2), uu = mul_f32x2(u, u);
+                        float u0, u1;
+                        unpack_f32x2(uu, u0, u1);
+                        top_u = fmaxf(top_u, fmaxf(u0, u1));
+                        y = fma_f32x2(mul_f32x2(raw, c1c1), tanh_ratio(uu), a);
+                    } else {
+                        y = fma_f32x2(raw, c1c1, a);
+                    }
+                    unpack_f32x2(y, x[i], x[i + 1]);
+                    if constexpr (kSlope)
+                        if (mixed) {
+                            x[i] = fmaf(-slope2, fabsf((float)(kv0 + col + i - q)), x[i]);
+                            x[i + 1] = fmaf(-slope2, fabsf((float)(kv0 + col + i + 1 - q)), x[i + 1]);
+                        }
+                }
+            };
+
+            for (;;) {
+                if (exact) {
+                    // ---- classical way: tile maximum, new reference, rescale of l and O ----
+                    float mx = -INFINITY;
+                    auto max_chunk = [&](int c, const uint32_t (&sr)[kCW]) {
+#pragma unroll
+                        for (int e = 0; e < kCW; e += 8) {
+                            float x[8];
+                            scores8(sr + e, c * kCW + e, 0.f, Tag<true>{}, x);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                if (c * kCW + e + i < valid) mx = fmaxf(mx, x[i]);
+                        }
+                    };
+                    if (!loaded) load_chunk(0, sa);
+                    tmem_wait_ld(); load_chunk(1, sb); max_chunk(0, sa);
+                    tmem_wait_ld(); load_chunk(2, sa); max_chunk(1, sb);
+                    tmem_wait_ld(); load_chunk(3, sb); max_chunk(2, sa);
+                    tmem_wait_ld(); max_chunk(3, sb);
+                    loaded = false;
+                    xchg[hf * 128 + r] = mx;
+                    named_barrier_sync(pair_bar, 64);
+                    mx = fmaxf(mx, xchg[(hf ^ 1) * 128 + r]);
+                    const float m_new = own == 0 ? ceilf(mx) : fmaxf(m, ceilf(mx));
+                    const float alpha = own == 0 ? 0.f : ex2_approx(m - m_new);      // (there is nothing yet; a first reference far below 0 would give infinity)
+                    l *= alpha;
+                    if (own > 0) {
+                        mbar_wait(bar(kBarODone + 2 * t + ((own - 1) & 1)), ((own - 1) >> 1) & 1, abort_flag, p.status, 251);
+                        tc_fence_after();
+                        uint32_t o[kOC];
+                        if constexpr (kOC == 32) tmem_ld32(tO, o); else tmem_ld16(tO, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < kOC; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                        if constexpr (kOC == 32) tmem_st32(tO, o); else tmem_st16(tO, o);
+                    }
+                    m = m_new;
+                }
+
+                // ---- P = 2^(score - m), row sum ----
+                uint64_t sum2 = pack_f32x2(0.f, 0.f);
+                auto exp_chunk = [&](int c, const uint32_t (&sr)[kCW], auto rag, auto far) {
+#pragma unroll
+                    for (int e = 0; e < kCW; e += 8) {
+                        float x[8];
+                        scores8(sr + e, c * kCW + e, -m, far, x);
+#pragma unroll
+                        for (int i = 0; i < 8; i += 2) {
+                            if constexpr (decltype(rag)::value) {
+                                if (c * kCW + e + i >= valid) x[i] = -INFINITY;
+                                if (c * kCW + e + i + 1 >= valid) x[i + 1] = -INFINITY;
+                            }
+                            const float lo = ex2_approx(x[i]), hi = ex2_approx(x[i + 1]);
+                            sum2 = add_f32x2(sum2, pack_f32x2(lo, hi));
+                            pk[(c * kCW + e + i) >> 1] = pack_bf16x2(lo, hi);
+                        }
+                    }
+                };
+                auto exp_pass = [&](auto rag, auto far) {
+                    if (!loaded) load_chunk(0, sa);
+                    tmem_wait_ld(); load_chunk(1, sb); exp_chunk(0, sa, rag, far);
+                    tmem_wait_ld(); load_chunk(2, sa); exp_chunk(1, sb, rag, far);
+                    tmem_wait_ld(); load_chunk(3, sb); exp_chunk(2, sa, rag, far);
+                    tmem_wait_ld(); exp_chunk(3, sb, rag, far);
+                };
+                if (kCap && (exact || wide)) exp_pass(Tag<true>{}, Tag<kCap>{});
+                else if (ragged) exp_pass(Tag<true>{}, Tag<false>{});
+                else exp_pass(Tag<false>{}, Tag<false>{});
+                loaded = false;
+                {
+                    float lo, hi;
+                    unpack_f32x2(sum2, lo, hi);
+                    tile_sum = lo + hi;
+                }
+                if (exact) break;
+                // reference too low for some row of this pair of warps?  Also catches inf / NaN, and scores near the cap.
+                const bool beyond = kCap && !wide && !(top_u <= kTanhReach);
+                if (!named_barrier_or(pair_bar, 64, !(tile_sum <= kSumThreshold) || beyond)) break;
+                if (kCap && !wide && named_barrier_or(pair_bar, 64, beyond)) wide = true;       // from now on, with the tanh of any score
+                else exact = true;
+            }
+            l += tile_sum;
+
+            // P over the first half of this thread's own score columns
+            tmem_st32(tS, pk);
+            tmem_wait_st();
+            tc_fence_before();
+            // Warps of a tile can be one step apart (nothing in the speculative pass waits for the previous PV MMA), so odd and even steps
+            // have barriers of their own: a parity wait can only tell two states apart.  Two steps apart is impossible, because the S MMA
+            // needs a score buffer that is only freed after the PV MMA.
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(kBarPFull + 2 * t + (own & 1)));
+            if (s + 1 < n_kv) begin_step(s + 1);
+        }
+
+        // ---- epilogue: O / l, LSE ----
+        const int last = n_kv - 1 - first;
+        mbar_wait(bar(kBarODone + 2 * t + (last & 1)), (last >> 1) & 1, abort_flag, p.status, 252);
+        tc_fence_after();
+        xchg[256 + hf * 128 + r] = l;
+        named_barrier_sync(pair_bar, 64);
+        l += xchg[256 + (hf ^ 1) * 128 + r];
+        const float inv_l = 1.0f / l;
+        uint32_t o[kOC];
+        if constexpr (kOC == 32) tmem_ld32(tO, o); else tmem_ld16(tO, o);
+        tmem_wait_ld();
+        if (q < n) {
+            uint4* dst = (uint4*)(p.out + ((size_t)(node0 + q) * p.n_heads + h) * D + hf * kOC);
+#pragma unroll
+            for (int i = 0; i < kOC / 8; ++i) {
+                uint4 v;
+                v.x = pack_bf16x2(__uint_as_float(o[8 * i]) * inv_l, __uint_as_float(o[8 * i + 1]) * inv_l);
+                v.y = pack_bf16x2(__uint_as_float(o[8 * i + 2]) * inv_l, __uint_as_float(o[8 * i + 3]) * inv_l);
+                v.z = pack_bf16x2(__uint_as_float(o[8 * i + 4]) * inv_l, __uint_as_float(o[8 * i + 5]) * inv_l);
+                v.w = pack_bf16x2(__uint_as_float(o[8 * i + 6]) * inv_l, __uint_as_float(o[8 * i + 7]) * inv_l);
+                dst[i] = v;
+            }
+            if (hf == 0) p.lse[(size_t)h * p.n_total + node0 + q] = (m + log2f(l)) * kLn2;
+        }
+    }
+
+    // ---- teardown ----
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag) __nanosleep(200000);    // let copies that may still be in flight land
+    if (warp == 1) tmem_dealloc(tmem, 512);
+}
+
+// Work list of a packed batch, a warp per document.
+constexpr int kListThreads = 128;
+__global__ void __launch_bounds__(kListThreads) position_list_kernel(int4* list, int32_t entries, const int32_t* cu_seqlens, int32_t n_graphs)
+{
+    grid_wait();
+    grid_release();
+    const int32_t w = (int32_t)((blockIdx.x * blockDim.x + threadIdx.x) >> 5);
+    if (w < n_graphs) write_work_list<2 * kTile>(list, entries, cu_seqlens, n_graphs, w);
+}
+constexpr size_t kListMinSaved = 2048;       // blocks of the plain grid that the list has to save: it costs a launch
+
+template <int D, bool kCap, bool kSlope>
+gt_status launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, PositionFwdParams p, const gt_batch* batch, int32_t rows,
+                 cudaStream_t s)
+{
+    const bool one = rows == kTile;
+    auto kern = one ? position_fwd_kernel<D, kCap, kSlope, 1> : position_fwd_kernel<D, kCap, kSlope, 2>;
+    static std::atomic<uint64_t> granted[2] = {};
+    const gt_status st = grant_smem(kern, granted[one], Smem<D>::kDynamic);
+    if (st != GT_OK) return st;
+    const dim3 grid = p.list ? dim3((unsigned)(list_entries(batch, rows) * p.n_heads))
+                             : dim3((unsigned)p.n_heads, (unsigned)((batch->max_seqlen + rows - 1) / rows), (unsigned)batch->n_graphs);
+    p.early_release = (int64_t)grid.x * grid.y * grid.z <= sm_count();
+    return launch_overlapped(kern, grid, 128 + 2 * rows, Smem<D>::kDynamic, s, tq, tk, tv, p);
+}
+
+}  // namespace
+}  // namespace gt
+
+extern "C" size_t gt_position_attn_fwd_workspace(const gt_batch* batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim)
+{
+    if (gt::position::validate(batch, n_heads, n_kv_heads, head_dim, nullptr, 0, 0.f) != GT_OK) return 0;
+    return gt::kHeaderBytes + gt::list_bytes(batch, 2 * gt::kTile);
+}
+
+extern "C" gt_status gt_position_attn_fwd(const void* q, const void* k, const void* v, const float* slopes, const int32_t* prefix,
+                                          const gt_batch* batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                          const gt_row_strides* strides, int32_t causal, float cap, void* out, float* lse,
+                                          void* workspace, size_t workspace_bytes, void* stream)
+{
+    using namespace gt;
+    gt_status st = position::validate(batch, n_heads, n_kv_heads, head_dim, prefix, causal, cap);
+    if (st != GT_OK) return st;
+    if (!q || !k || !v || !out || !lse) return GT_ERR_INVALID_ARG;
+    if (misaligned16(q) || misaligned16(k) || misaligned16(v) || misaligned16(out)) return GT_ERR_INVALID_ARG;
+    int64_t sq, sk, sv;
+    if (!position::row_stride(strides ? strides->q : 0, n_heads, head_dim, &sq) || !position::row_stride(strides ? strides->k : 0, n_kv_heads, head_dim, &sk) ||
+        !position::row_stride(strides ? strides->v : 0, n_kv_heads, head_dim, &sv))
+        return GT_ERR_INVALID_ARG;
+    if (workspace == nullptr || misaligned16(workspace) || workspace_bytes < gt_position_attn_fwd_workspace(batch, n_heads, n_kv_heads, head_dim))
+        return GT_ERR_WORKSPACE;
+    if (sm_count() <= 0) return GT_ERR_NO_DEVICE;
+    CUtensorMap tq, tk, tv;
+    if ((st = encode_rows_map(&tq, q, batch->n_total, n_heads, head_dim, sq)) != GT_OK) return st;
+    if ((st = encode_rows_map(&tk, k, batch->n_total, n_kv_heads, head_dim, sk)) != GT_OK) return st;
+    if ((st = encode_rows_map(&tv, v, batch->n_total, n_kv_heads, head_dim, sv)) != GT_OK) return st;
+    PositionFwdParams p{};
+    p.cu_seqlens = batch->cu_seqlens;
+    p.prefix = prefix;
+    p.slopes = slopes;
+    p.out = (__nv_bfloat16*)out;
+    p.lse = lse;
+    p.status = (uint32_t*)workspace;
+    p.n_total = batch->n_total;
+    p.n_heads = n_heads;
+    p.group = n_heads / n_kv_heads;
+    p.causal = causal != 0;
+    p.c1 = kLog2e / sqrtf((float)head_dim);
+    p.to_tanh = cap > 0.f ? 1.0f / (sqrtf((float)head_dim) * cap) : 0.f;
+    p.cap2 = cap * kLog2e;
+    cudaStream_t s = (cudaStream_t)stream;
+    // Blocks of one query tile where those of two would leave half of the SMs idle or more.
+    const int32_t rows = (int64_t)((batch->max_seqlen + kTile - 1) / kTile) * batch->n_graphs * n_heads <= sm_count() ? kTile : 2 * kTile;
+    if (batch->n_graphs > 1 && rows == 2 * kTile && list_saves(batch, rows, n_heads, kListMinSaved)) {
+        int4* list = (int4*)((uint8_t*)workspace + kHeaderBytes);
+        p.list = list;
+        const unsigned blocks = (unsigned)((batch->n_graphs + kListThreads / 32 - 1) / (kListThreads / 32));
+        if ((st = launch_overlapped(position_list_kernel, dim3(blocks), kListThreads, 0, s, list, (int32_t)list_entries(batch, rows), batch->cu_seqlens,
+                                    batch->n_graphs)) != GT_OK)
+            return st;
+    }
+    auto go = [&](auto d, auto capped) {
+        constexpr int D = decltype(d)::value ? 64 : 32;
+        return slopes ? launch<D, decltype(capped)::value, true>(tq, tk, tv, p, batch, rows, s)
+                      : launch<D, decltype(capped)::value, false>(tq, tk, tv, p, batch, rows, s);
+    };
+    if (head_dim == 64) return cap > 0.f ? go(Tag<true>{}, Tag<true>{}) : go(Tag<true>{}, Tag<false>{});
+    return cap > 0.f ? go(Tag<false>{}, Tag<true>{}) : go(Tag<false>{}, Tag<false>{});
+}
