@@ -145,11 +145,11 @@ def lib() -> ctypes.CDLL:
         L.gt_position_attn_fwd_workspace.restype = sz
         L.gt_position_attn_fwd_workspace.argtypes = [bp, i32, i32, i32]
         L.gt_position_attn_fwd.restype = ctypes.c_int
-        L.gt_position_attn_fwd.argtypes = [vp] * 5 + [bp, i32, i32, i32, sp, i32, f32, vp, vp, vp, sz, vp]
+        L.gt_position_attn_fwd.argtypes = [vp] * 5 + [bp, i32, i32, i32, sp, i32, f32, vp, vp, vp, vp, sz, vp]
         L.gt_position_attn_bwd_workspace.restype = sz
         L.gt_position_attn_bwd_workspace.argtypes = [bp, i32, i32, i32]
         L.gt_position_attn_bwd.restype = ctypes.c_int
-        L.gt_position_attn_bwd.argtypes = [vp] * 8 + [bp, i32, i32, i32, sp, i32, f32, vp, vp, vp, vp, sz, vp]
+        L.gt_position_attn_bwd.argtypes = [vp] * 9 + [bp, i32, i32, i32, sp, i32, f32, vp, vp, vp, vp, sz, vp]
         L.gt_rotary.restype = ctypes.c_int
         L.gt_rotary.argtypes = [vp] * 4 + [bp] + [i32] * 6 + [f32, i32] + [i64] * 4 + [vp, vp, vp]
         L.gt_rotary_frequencies.restype = ctypes.c_int
@@ -557,16 +557,20 @@ def _position_strides(q, k, v, dq=None, dk=None, dv=None):
 
 
 def gt_position_attn_fwd(q, k, v, slopes: Optional[torch.Tensor], prefix: Optional[torch.Tensor], batch: Batch,
-                         causal: bool, cap: float, out, lse, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """Attention over token sequences: q [T, H, d], k and v [T, G, d] (rows may lie apart), slopes fp32 [H], prefix int32 [documents]."""
+                         causal: bool, cap: float, out, lse, out_f32: Optional[torch.Tensor] = None,
+                         workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention over token sequences: q [T, H, d], k and v [T, G, d] (rows may lie apart), slopes fp32 [H], prefix int32 [documents];
+    ``out_f32``, fp32 [T, H, d], is the output before its rounding, for an exact backward."""
     _, H, d = q.shape
     G = k.shape[1]
     _same_dtype(torch.bfloat16, q, k, v, out)
+    _same_dtype(torch.float32, slopes, lse, out_f32)
+    _same_dtype(torch.int32, prefix)
     if workspace is None:
         workspace = _workspace(gt_position_attn_fwd_workspace(batch, H, G, d), q.device)
     strides, (pq, pk, pv, _, _, _) = _position_strides(q, k, v)
     st = lib().gt_position_attn_fwd(pq, pk, pv, _ptr(slopes), _ptr(prefix), batch._c_pair()[1], H, G, d, ctypes.byref(strides),
-                                    int(causal), float(cap), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel(), _stream())
+                                    int(causal), float(cap), _ptr(out), _ptr(lse), _ptr(out_f32), _ptr(workspace), workspace.numel(), _stream())
     _raise(st, "gt_position_attn_fwd")
     return workspace
 
@@ -577,15 +581,18 @@ def gt_position_attn_bwd_workspace(batch: Batch, n_heads: int, n_kv_heads: int, 
 
 
 def gt_position_attn_bwd(q, k, v, out, dout, lse, slopes: Optional[torch.Tensor], prefix: Optional[torch.Tensor], batch: Batch,
-                         causal: bool, cap: float, dq, dk, dv, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """Gradients of gt_position_attn_fwd; rows of q, k, v, dq, dk and dv may lie apart."""
+                         causal: bool, cap: float, dq, dk, dv, out_f32: Optional[torch.Tensor] = None,
+                         workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradients of gt_position_attn_fwd; rows of q, k, v, dq, dk and dv may lie apart.  ``out`` may be None beside ``out_f32``."""
     _, H, d = q.shape
     G = k.shape[1]
     _same_dtype(torch.bfloat16, q, k, v, out, dout, dq, dk, dv)
+    _same_dtype(torch.float32, slopes, lse, out_f32)
+    _same_dtype(torch.int32, prefix)
     if workspace is None:
         workspace = _workspace(gt_position_attn_bwd_workspace(batch, H, G, d), q.device)
     strides, (pq, pk, pv, pdq, pdk, pdv) = _position_strides(q, k, v, dq, dk, dv)
-    st = lib().gt_position_attn_bwd(pq, pk, pv, _ptr(out), _ptr(dout), _ptr(lse), _ptr(slopes), _ptr(prefix), batch._c_pair()[1],
+    st = lib().gt_position_attn_bwd(pq, pk, pv, _ptr(out), _ptr(out_f32), _ptr(dout), _ptr(lse), _ptr(slopes), _ptr(prefix), batch._c_pair()[1],
                                     H, G, d, ctypes.byref(strides), int(causal), float(cap), pdq, pdk, pdv,
                                     _ptr(workspace), workspace.numel(), _stream())
     _raise(st, "gt_position_attn_bwd")

@@ -47,6 +47,15 @@ __device__ __forceinline__ float tanh_any(float y)
 // A query at position i of a document of n tokens sees the document's keys [0, row_limit).
 __device__ __forceinline__ int32_t row_limit(bool causal, int32_t i, int32_t prefix, int32_t n) { return causal ? min(n, max(i + 1, prefix)) : n; }
 
+// go(Tag<wide>, Tag<capped>, Tag<sloped>) for three values that are known when the program runs.
+template <typename Go>
+gt_status pick(bool wide, bool capped, bool sloped, Go go)
+{
+    auto third = [&](auto a, auto b) { return sloped ? go(a, b, Tag<true>{}) : go(a, b, Tag<false>{}); };
+    auto second = [&](auto a) { return capped ? third(a, Tag<true>{}) : third(a, Tag<false>{}); };
+    return wide ? second(Tag<true>{}) : second(Tag<false>{});
+}
+
 constexpr float kMaxCap = 1e6f;
 constexpr int64_t kMaxRowStride = (int64_t)1 << 38;
 

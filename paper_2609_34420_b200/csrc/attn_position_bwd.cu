@@ -560,6 +560,7 @@ __device__ __forceinline__ void split3_bf16(float v, uint32_t& w01, uint32_t& w2
 
 struct PrepareParams {
     const __nv_bfloat16* out;
+    const float* out_f32;      // the forward's output before its rounding, where the caller has it (then instead of `out`)
     const __nv_bfloat16* dout;
     const float* lse;
     uint4* ext;
@@ -582,7 +583,7 @@ template <int D>
 __global__ void __launch_bounds__(kPrepareThreads) position_prepare_kernel(const PrepareParams p)
 {
     constexpr int kChunks = D / 8, kSwz = kChunks - 1;
-    __shared__ __align__(16) uint8_t s_do[kPrepareRows * 2 * D], s_o[kPrepareRows * 2 * D];
+    __shared__ __align__(16) uint8_t s_do[kPrepareRows * 2 * D], s_o[kPrepareRows * 4 * D];
     grid_wait();
     grid_release();
     if (blockIdx.x >= p.row_blocks) {
@@ -592,25 +593,26 @@ __global__ void __launch_bounds__(kPrepareThreads) position_prepare_kernel(const
     }
     const size_t n_rows = (size_t)p.n_total * p.n_heads, row0 = (size_t)blockIdx.x * kPrepareRows;
     const int rows = (int)(row0 + kPrepareRows < n_rows ? kPrepareRows : n_rows - row0);
-    const uint4* from_do = (const uint4*)p.dout + row0 * kChunks;
-    const uint4* from_o = (const uint4*)p.out + row0 * kChunks;
-    constexpr int kEach = kPrepareRows * kChunks / kPrepareThreads;
-    uint4 x[kEach], y[kEach];
+    auto stage = [&](uint8_t* dst, const void* src, auto chunks_) {
+        constexpr int chunks = decltype(chunks_)::value ? 2 * kChunks : kChunks, kEach = kPrepareRows * chunks / kPrepareThreads;
+        const uint4* from = (const uint4*)src + row0 * chunks;
+        uint4 x[kEach];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const int e = (int)threadIdx.x + i * kPrepareThreads;
-        if (e < rows * kChunks) { x[i] = from_do[e]; y[i] = from_o[e]; }
-    }
+        for (int i = 0; i < kEach; ++i) {
+            const int e = (int)threadIdx.x + i * kPrepareThreads;
+            if (e < rows * chunks) x[i] = from[e];
+        }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int e = (int)threadIdx.x + i * kPrepareThreads, r = e / chunks, c = e % chunks;
+            if (e < rows * chunks) *(uint4*)(dst + r * chunks * 16 + ((c ^ (r & kSwz)) << 4)) = x[i];
+        }
+    };
     for (size_t i = (size_t)blockIdx.x * kPrepareThreads + threadIdx.x; i < p.n_acc; i += (size_t)p.row_blocks * kPrepareThreads)
         p.acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const int e = (int)threadIdx.x + i * kPrepareThreads, r = e / kChunks, c = e % kChunks;
-        if (e < rows * kChunks) {
-            *(uint4*)(s_do + r * 2 * D + ((c ^ (r & kSwz)) << 4)) = x[i];
-            *(uint4*)(s_o + r * 2 * D + ((c ^ (r & kSwz)) << 4)) = y[i];
-        }
-    }
+    stage(s_do, p.dout, Tag<false>{});
+    if (p.out_f32 != nullptr) stage(s_o, p.out_f32, Tag<true>{});
+    else stage(s_o, p.out, Tag<false>{});
     __syncthreads();
     const int r = (int)threadIdx.x;
     if (r >= rows) return;
@@ -618,12 +620,25 @@ __global__ void __launch_bounds__(kPrepareThreads) position_prepare_kernel(const
     float acc = 0.f;
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
-        const uint4 b = *(const uint4*)(s_do + r * 2 * D + ((i ^ (r & kSwz)) << 4)), a = *(const uint4*)(s_o + r * 2 * D + ((i ^ (r & kSwz)) << 4));
-        const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+        const uint4 b = *(const uint4*)(s_do + r * 2 * D + ((i ^ (r & kSwz)) << 4));
+        const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
+        if (p.out_f32 != nullptr) {
+            const float4 a0 = *(const float4*)(s_o + r * 4 * D + (((2 * i) ^ (r & kSwz)) << 4));
+            const float4 a1 = *(const float4*)(s_o + r * 4 * D + (((2 * i + 1) ^ (r & kSwz)) << 4));
+            const float a[8] = {a0.x, a0.y, a0.z, a0.w, a1.x, a1.y, a1.z, a1.w};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            acc += __uint_as_float(aw[k] << 16) * __uint_as_float(bw[k] << 16);
-            acc += __uint_as_float(aw[k] & 0xffff0000u) * __uint_as_float(bw[k] & 0xffff0000u);
+            for (int k = 0; k < 4; ++k) {
+                acc += a[2 * k] * __uint_as_float(bw[k] << 16);
+                acc += a[2 * k + 1] * __uint_as_float(bw[k] & 0xffff0000u);
+            }
+        } else {
+            const uint4 a = *(const uint4*)(s_o + r * 2 * D + ((i ^ (r & kSwz)) << 4));
+            const uint32_t aw[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                acc += __uint_as_float(aw[k] << 16) * __uint_as_float(bw[k] << 16);
+                acc += __uint_as_float(aw[k] & 0xffff0000u) * __uint_as_float(bw[k] & 0xffff0000u);
+            }
         }
     }
     uint4 e0 = make_uint4(0u, 0u, 0u, 0u), e1 = make_uint4(0u, 0u, 0u, 0u);
@@ -707,8 +722,8 @@ extern "C" size_t gt_position_attn_bwd_workspace(const gt_batch* batch, int32_t 
     return gt::workspace_of(batch, n_heads, n_kv_heads, head_dim).total;
 }
 
-extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const void* v, const void* out, const void* dout, const float* lse,
-                                          const float* slopes, const int32_t* prefix,
+extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const void* v, const void* out, const float* out_f32,
+                                          const void* dout, const float* lse, const float* slopes, const int32_t* prefix,
                                           const gt_batch* batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                                           const gt_row_strides* strides, int32_t causal, float cap,
                                           void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes, void* stream)
@@ -716,8 +731,8 @@ extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const vo
     using namespace gt;
     gt_status st = position::validate(batch, n_heads, n_kv_heads, head_dim, prefix, causal, cap);
     if (st != GT_OK) return st;
-    if (!q || !k || !v || !out || !dout || !lse || !dq || !dk || !dv) return GT_ERR_INVALID_ARG;
-    if (misaligned16(q) || misaligned16(k) || misaligned16(v) || misaligned16(out) || misaligned16(dout) || misaligned16(dq) || misaligned16(dk) ||
+    if (!q || !k || !v || (!out && !out_f32) || !dout || !lse || !dq || !dk || !dv) return GT_ERR_INVALID_ARG;
+    if (misaligned16(q) || misaligned16(k) || misaligned16(v) || misaligned16(out) || misaligned16(out_f32) || misaligned16(dout) || misaligned16(dq) || misaligned16(dk) ||
         misaligned16(dv))
         return GT_ERR_INVALID_ARG;
     const gt_row_strides given = strides ? *strides : gt_row_strides{};
@@ -765,6 +780,7 @@ extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const vo
 
     PrepareParams pre{};
     pre.out = (const __nv_bfloat16*)out;
+    pre.out_f32 = out_f32;
     pre.dout = (const __nv_bfloat16*)dout;
     pre.lse = lse;
     pre.ext = (uint4*)(ws + w.ext_off);
@@ -781,12 +797,9 @@ extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const vo
     auto prepare = head_dim == 64 ? position_prepare_kernel<64> : position_prepare_kernel<32>;
     if ((st = launch_overlapped(prepare, dim3(pre.row_blocks + list_blocks), kPrepareThreads, 0, s, pre)) != GT_OK) return st;
 
-    auto go = [&](auto d, auto capped) {
-        constexpr int D = decltype(d)::value ? 64 : 32;
-        return slopes ? launch<D, decltype(capped)::value, true>(maps, p, batch, s) : launch<D, decltype(capped)::value, false>(maps, p, batch, s);
-    };
-    if (head_dim == 64) st = cap > 0.f ? go(Tag<true>{}, Tag<true>{}) : go(Tag<true>{}, Tag<false>{});
-    else st = cap > 0.f ? go(Tag<false>{}, Tag<true>{}) : go(Tag<false>{}, Tag<false>{});
+    st = position::pick(head_dim == 64, cap > 0.f, slopes != nullptr, [&](auto wide, auto capped, auto sloped) {
+        return launch<decltype(wide)::value ? 64 : 32, decltype(capped)::value, decltype(sloped)::value>(maps, p, batch, s);
+    });
     if (st != GT_OK) return st;
 
     FinishParams f{};

@@ -42,6 +42,7 @@ struct PositionFwdParams {
     const int32_t* prefix;
     const float* slopes;
     __nv_bfloat16* out;        // [T,H,D]
+    float* out_f32;            // [T,H,D] fp32, or nullptr
     float* lse;                // [H,T]
     uint32_t* status;
     const int4* list;          // packed batch: work list; block index = entry * heads + head (nullptr: grid of heads x blocks x documents)
@@ -84,7 +85,11 @@ struct Smem {
 constexpr int kNbPair = 2;                    // named barriers: + 4 t + lane quarter, the two warps that share 32 query rows
 
 // kTiles = 1: blocks of one query tile, for grids that would leave half of the SMs idle or more.
-template <int D, bool kCap, bool kSlope, int kTiles>
+// kExact (with the fp32 output): O is divided by the sum of the probabilities as the MMA reads them, rounded to bf16, so that their
+// rounding cancels where a row has few large ones; lse is that of the unrounded ones all the same.  The backward subtracts dout . out from
+// dout . v_j, two nearly equal numbers in such rows: with scores of standard deviation 4, dq was off by 0.6 % (out rounded to bf16 and
+// divided by the unrounded sum), by 0.45 % without either, and by 0.27 % with both.
+template <int D, bool kCap, bool kSlope, int kTiles, bool kExact>
 __global__ void __launch_bounds__(128 + 256 * kTiles, 1)
 position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                     const __grid_constant__ CUtensorMap tmap_v, const PositionFwdParams p)
@@ -249,6 +254,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         const int32_t least_limit = row_limit(p.causal, q0 + t * kTile + (warp & 3) * 32, prefix, n);        // of the warp's rows
         const int32_t first = t == 0 ? skip : 0;
         float m = 0.f, l = 0.f;
+        [[maybe_unused]] float l_rounded = 0.f;
         bool wide = false;                               // kCap: a score was out of the polynomial's reach
         const uint64_t c1c1 = both(p.c1);
         [[maybe_unused]] const uint64_t to_tanh2 = both(p.to_tanh);
@@ -281,6 +287,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             [[maybe_unused]] const float step_slope = before ? slope2 : -slope2;
             uint32_t pk[32];                       // P of this thread's columns, bf16 pairs
             float tile_sum = 0.f;
+            [[maybe_unused]] uint64_t rounded2 = 0;
             bool loaded = true;                    // chunk 0 is already on its way
             bool exact = false;                    // take the tile maximum first
 
@@ -359,6 +366,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     const float m_new = own == 0 ? ceilf(mx) : fmaxf(m, ceilf(mx));
                     const float alpha = own == 0 ? 0.f : ex2_approx(m - m_new);      // (there is nothing yet; a first reference far below 0 would give infinity)
                     l *= alpha;
+                    if constexpr (kExact) l_rounded *= alpha;
                     if (own > 0) {
                         mbar_wait(bar(kBarODone + 2 * t + ((own - 1) & 1)), ((own - 1) >> 1) & 1, abort_flag, p.status, 251);
                         tc_fence_after();
@@ -374,6 +382,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 
                 // ---- P = 2^(score - m), row sum ----
                 uint64_t sum2 = pack_f32x2(0.f, 0.f);
+                rounded2 = sum2;
                 auto exp_chunk = [&](int c, const uint32_t (&sr)[kCW], auto rag, auto far) {
 #pragma unroll
                     for (int e = 0; e < kCW; e += 8) {
@@ -387,7 +396,8 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                             }
                             const float lo = ex2_approx(x[i]), hi = ex2_approx(x[i + 1]);
                             sum2 = add_f32x2(sum2, pack_f32x2(lo, hi));
-                            pk[(c * kCW + e + i) >> 1] = pack_bf16x2(lo, hi);
+                            const uint32_t w = pk[(c * kCW + e + i) >> 1] = pack_bf16x2(lo, hi);
+                            if constexpr (kExact) rounded2 = add_f32x2(rounded2, pack_u32x2(w << 16, w & 0xffff0000u));
                         }
                     }
                 };
@@ -415,6 +425,11 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 else exact = true;
             }
             l += tile_sum;
+            if constexpr (kExact) {
+                float lo, hi;
+                unpack_f32x2(rounded2, lo, hi);
+                l_rounded += lo + hi;
+            }
 
             // P over the first half of this thread's own score columns
             tmem_st32(tS, pk);
@@ -433,9 +448,11 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         mbar_wait(bar(kBarODone + 2 * t + (last & 1)), (last >> 1) & 1, abort_flag, p.status, 252);
         tc_fence_after();
         xchg[256 + hf * 128 + r] = l;
+        if constexpr (kExact) xchg[hf * 128 + r] = l_rounded;
         named_barrier_sync(pair_bar, 64);
         l += xchg[256 + (hf ^ 1) * 128 + r];
-        const float inv_l = 1.0f / l;
+        if constexpr (kExact) l_rounded += xchg[(hf ^ 1) * 128 + r];
+        const float inv_l = 1.0f / (kExact ? l_rounded : l);
         uint32_t o[kOC];
         if constexpr (kOC == 32) tmem_ld32(tO, o); else tmem_ld16(tO, o);
         tmem_wait_ld();
@@ -449,6 +466,13 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 v.z = pack_bf16x2(__uint_as_float(o[8 * i + 4]) * inv_l, __uint_as_float(o[8 * i + 5]) * inv_l);
                 v.w = pack_bf16x2(__uint_as_float(o[8 * i + 6]) * inv_l, __uint_as_float(o[8 * i + 7]) * inv_l);
                 dst[i] = v;
+            }
+            if constexpr (kExact) {
+                float4* dst32 = (float4*)(p.out_f32 + ((size_t)(node0 + q) * p.n_heads + h) * D + hf * kOC);
+#pragma unroll
+                for (int i = 0; i < kOC / 4; ++i)
+                    dst32[i] = make_float4(__uint_as_float(o[4 * i]) * inv_l, __uint_as_float(o[4 * i + 1]) * inv_l,
+                                           __uint_as_float(o[4 * i + 2]) * inv_l, __uint_as_float(o[4 * i + 3]) * inv_l);
             }
             if (hf == 0) p.lse[(size_t)h * p.n_total + node0 + q] = (m + log2f(l)) * kLn2;
         }
@@ -472,12 +496,12 @@ __global__ void __launch_bounds__(kListThreads) position_list_kernel(int4* list,
 }
 constexpr size_t kListMinSaved = 2048;       // blocks of the plain grid that the list has to save: it costs a launch
 
-template <int D, bool kCap, bool kSlope>
+template <int D, bool kCap, bool kSlope, bool kExact>
 gt_status launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, PositionFwdParams p, const gt_batch* batch, int32_t rows,
                  cudaStream_t s)
 {
     const bool one = rows == kTile;
-    auto kern = one ? position_fwd_kernel<D, kCap, kSlope, 1> : position_fwd_kernel<D, kCap, kSlope, 2>;
+    auto kern = one ? position_fwd_kernel<D, kCap, kSlope, 1, kExact> : position_fwd_kernel<D, kCap, kSlope, 2, kExact>;
     static std::atomic<uint64_t> granted[2] = {};
     const gt_status st = grant_smem(kern, granted[one], Smem<D>::kDynamic);
     if (st != GT_OK) return st;
@@ -498,14 +522,14 @@ extern "C" size_t gt_position_attn_fwd_workspace(const gt_batch* batch, int32_t 
 
 extern "C" gt_status gt_position_attn_fwd(const void* q, const void* k, const void* v, const float* slopes, const int32_t* prefix,
                                           const gt_batch* batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
-                                          const gt_row_strides* strides, int32_t causal, float cap, void* out, float* lse,
+                                          const gt_row_strides* strides, int32_t causal, float cap, void* out, float* lse, float* out_f32,
                                           void* workspace, size_t workspace_bytes, void* stream)
 {
     using namespace gt;
     gt_status st = position::validate(batch, n_heads, n_kv_heads, head_dim, prefix, causal, cap);
     if (st != GT_OK) return st;
     if (!q || !k || !v || !out || !lse) return GT_ERR_INVALID_ARG;
-    if (misaligned16(q) || misaligned16(k) || misaligned16(v) || misaligned16(out)) return GT_ERR_INVALID_ARG;
+    if (misaligned16(q) || misaligned16(k) || misaligned16(v) || misaligned16(out) || misaligned16(out_f32)) return GT_ERR_INVALID_ARG;
     int64_t sq, sk, sv;
     if (!position::row_stride(strides ? strides->q : 0, n_heads, head_dim, &sq) || !position::row_stride(strides ? strides->k : 0, n_kv_heads, head_dim, &sk) ||
         !position::row_stride(strides ? strides->v : 0, n_kv_heads, head_dim, &sv))
@@ -522,6 +546,7 @@ extern "C" gt_status gt_position_attn_fwd(const void* q, const void* k, const vo
     p.prefix = prefix;
     p.slopes = slopes;
     p.out = (__nv_bfloat16*)out;
+    p.out_f32 = out_f32;
     p.lse = lse;
     p.status = (uint32_t*)workspace;
     p.n_total = batch->n_total;
@@ -542,11 +567,10 @@ extern "C" gt_status gt_position_attn_fwd(const void* q, const void* k, const vo
                                     batch->n_graphs)) != GT_OK)
             return st;
     }
-    auto go = [&](auto d, auto capped) {
-        constexpr int D = decltype(d)::value ? 64 : 32;
-        return slopes ? launch<D, decltype(capped)::value, true>(tq, tk, tv, p, batch, rows, s)
-                      : launch<D, decltype(capped)::value, false>(tq, tk, tv, p, batch, rows, s);
+    auto go = [&](auto wide, auto capped, auto sloped) {
+        constexpr int D = decltype(wide)::value ? 64 : 32;
+        constexpr bool kCap = decltype(capped)::value, kSlope = decltype(sloped)::value;
+        return out_f32 ? launch<D, kCap, kSlope, true>(tq, tk, tv, p, batch, rows, s) : launch<D, kCap, kSlope, false>(tq, tk, tv, p, batch, rows, s);
     };
-    if (head_dim == 64) return cap > 0.f ? go(Tag<true>{}, Tag<true>{}) : go(Tag<true>{}, Tag<false>{});
-    return cap > 0.f ? go(Tag<false>{}, Tag<true>{}) : go(Tag<false>{}, Tag<false>{});
+    return position::pick(head_dim == 64, cap > 0.f, slopes != nullptr, go);
 }

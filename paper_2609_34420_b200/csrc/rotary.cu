@@ -2,9 +2,8 @@
 //
 //     (a, b) -> scale (a cos w - b sin w, a sin w + b cos w),   w = position * frequency[pair]
 //
-// Bound by memory: every row is read and written once.  A warp has a token.  Lane i makes the cosine and sine of pair i (a head has 32
-// pairs at most), the lanes pass them on through shared memory, and then every lane keeps those of its own 16-byte pieces in registers
-// while it walks over the heads, 32 bytes at a time, of q and of k.
+// Bound by memory: every row is read and written once.  A block has some consecutive tokens: it makes the cosines and sines of their
+// pairs once for all heads, into shared memory, while its first rows are on their way, and then rotates 32 bytes of a head at a time.
 //
 // The angle is reduced in fp64: turns = position * frequency / 2 pi, less the next whole number, is off by 2^-52 of itself, 5e-7 rad at
 // position 2^31; in fp32 a position of a million would leave nothing of it.  What is left goes to sincospi in fp32.
@@ -28,11 +27,13 @@ struct RotaryParams {
     int32_t n_total, n_graphs;
     int32_t heads[2];
     int32_t rot_dim;
+    int32_t tokens;            // of a block
+    int32_t step_tokens, step_heads;       // from a thread's piece to its next: so many tokens and heads further
     int32_t copy;              // channels behind rot_dim have to be copied (some output is not in place)
     float scale, sin_scale;
 };
 
-constexpr int kThreads = 256, kTokens = kThreads / 32;
+constexpr int kThreads = 256, kMaxTokens = 32;
 constexpr double kTurn = 0.15915494309189533577;         // 1 / 2 pi
 
 template <typename T> __device__ __forceinline__ float widen(T v);
@@ -46,114 +47,110 @@ template <> __device__ __forceinline__ __half narrow(float v) { return __float2h
 
 template <typename T> struct alignas(16) Piece { T v[16 / sizeof(T)]; };
 
-// The document that token t belongs to: the last one that begins at or before it (those without tokens lie before); by whole warps.
+// First row of the document that row t belongs to: the last one that begins at or before it (those without rows lie before).
 __device__ __forceinline__ int32_t document_start(const int32_t* __restrict__ cu_seqlens, int32_t n_graphs, int32_t t)
 {
-    const int lane = threadIdx.x & 31;
-    int32_t lo = 0, n = n_graphs, start = 0;               // it is one of [lo, lo + n)
-    for (;;) {
-        const int32_t step = (n + 31) / 32, x = lane * step;
-        const int32_t begin = x < n ? cu_seqlens[lo + x] : 0x7fffffff;
-        const int32_t last = __popc(__ballot_sync(0xffffffffu, begin <= t)) - 1;          // (lane 0's begins there)
-        start = __shfl_sync(0xffffffffu, begin, last);
-        if (step == 1) return start;
-        lo += last * step;
-        n = min(step, n - last * step);
+    int32_t lo = 0, n = n_graphs;                          // it is one of [lo, lo + n)
+    while (n > 1) {
+        const int32_t step = n / 2;
+        if (cu_seqlens[lo + step] <= t) { lo += step; n -= step; } else n = step;
     }
+    return cu_seqlens[lo];
+}
+__device__ __forceinline__ int32_t position_of(const RotaryParams& p, int32_t t)
+{
+    return p.positions ? p.positions[t] : p.cu_seqlens ? t - document_start(p.cu_seqlens, p.n_graphs, t) : t;
 }
 
-// Cosine and sine of pair `lane` at token t, scaled.
-__device__ __forceinline__ float2 turn_of(const RotaryParams& p, int32_t t)
+// Cosine and sine of a pair at a position, scaled.
+__device__ __forceinline__ float2 turn_of(const RotaryParams& p, int32_t position, double frequency)
 {
-    const int lane = threadIdx.x & 31;
-    const int32_t position = p.positions ? p.positions[t] : p.cu_seqlens ? t - document_start(p.cu_seqlens, p.n_graphs, t) : t;
-    if (lane >= p.rot_dim / 2) return make_float2(1.f, 0.f);
-    double turns = (double)position * (p.frequencies[lane] * kTurn);
+    double turns = (double)position * (frequency * kTurn);
     turns -= rint(turns);
     float s, c;
     sincospif((float)(2.0 * turns), &s, &c);
     return make_float2(c * p.scale, s * p.sin_scale);
 }
 
-// Rows, and in the layout of halves the rotated channels of each half, come in whole pieces of 16 bytes.  A lane has the same two pieces of
-// every head that it meets: two neighbours, or (halves) the same piece of both halves.
+// Rows, and in the layout of halves the rotated channels of each half, come in whole pieces of 16 bytes.  A thread takes two pieces of a
+// head at a time: two neighbours, or (halves) the same piece of both halves.
 template <typename T, int D, bool kInterleaved>
 __global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryParams p)
 {
-    constexpr int kVec = 16 / sizeof(T), kUnits = D / (2 * kVec), kHeads = 32 / kUnits;       // elements of a piece, lanes per head, heads at a time
-    constexpr int kUnroll = 4;
-    __shared__ float2 s_turn[kTokens][D / 2];
+    constexpr int kVec = 16 / sizeof(T), kUnits = D / (2 * kVec);       // elements of a piece, pairs of pieces in a head
+    constexpr int kAhead = 2;
+    __shared__ int32_t s_position[kMaxTokens];
+    __shared__ __align__(16) float2 s_turn[kMaxTokens][D / 2];
     grid_wait();
     grid_release();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t t = (int64_t)blockIdx.x * kTokens + warp;
-    if (t >= p.n_total) return;
-    const int unit = lane % kUnits, all = p.heads[0] + p.heads[1];
-    const int half_pieces = p.rot_dim / 2 / kVec;             // halves: pieces per half
-    const bool rotated = kInterleaved ? unit * kVec < p.rot_dim / 2 : unit < half_pieces;
-    int at0, at1;                                              // first elements of the lane's pieces within a head
-    if (kInterleaved) { at0 = unit * 2 * kVec; at1 = at0 + kVec; }
-    else if (rotated) { at0 = unit * kVec; at1 = at0 + p.rot_dim / 2; }
-    else { at0 = p.rot_dim + (unit - half_pieces) * 2 * kVec; at1 = at0 + kVec; }
-    const bool mine = rotated || p.copy;
-    auto where = [&](int h, int64_t* from, int64_t* to) -> int {
-        const int of = h < p.heads[0] ? 0 : 1, head = h - (of ? p.heads[0] : 0);
-        *from = t * p.x_row[of] + (int64_t)head * D * (int)sizeof(T);
-        *to = t * p.y_row[of] + (int64_t)head * D * (int)sizeof(T);
-        return of;
+    const int tid = threadIdx.x, unit = tid % kUnits, all = p.heads[0] + p.heads[1], half = p.rot_dim / 2;
+    const int64_t t0 = (int64_t)blockIdx.x * p.tokens;
+    int tokens = (int)min((int64_t)p.tokens, (int64_t)p.n_total - t0);
+    const bool rotated = unit * kVec < half, mine = rotated || p.copy;
+    int at0 = unit * (kInterleaved ? 2 * kVec : kVec), at1 = kInterleaved ? at0 + kVec : at0 + half;      // the thread's pieces within a head
+    if (!kInterleaved && !rotated) {
+        at0 = p.rot_dim + (unit * kVec - half) * 2;
+        at1 = at0 + kVec;
+    }
+    Piece<T> a[kAhead], b[kAhead];
+    int token = tid / kUnits / all, head = tid / kUnits - token * all;        // of the next piece to load, and of the next to store
+    int out_token = token, out_head = head;
+    auto advance = [&](int& tk, int& hd) {
+        tk += p.step_tokens;
+        hd += p.step_heads;
+        if (hd >= all) { hd -= all; ++tk; }
     };
-    Piece<T> a[kUnroll], b[kUnroll];
-    auto load = [&](int h0) {
-#pragma unroll
-        for (int i = 0; i < kUnroll; ++i) {
-            const int h = h0 + i * kHeads;
-            if (h >= all || !mine) continue;
-            int64_t from, to;
-            const uint8_t* src = p.x[where(h, &from, &to)] + from;
-            a[i] = *(const Piece<T>*)(src + at0 * sizeof(T));
-            b[i] = *(const Piece<T>*)(src + at1 * sizeof(T));
+    auto load = [&](int i) {
+        if (mine && token < tokens) {
+            const bool second = head >= p.heads[0];
+            const uint8_t* src = (second ? p.x[1] : p.x[0]) + (t0 + token) * (second ? p.x_row[1] : p.x_row[0]) +
+                                 (head - (second ? p.heads[0] : 0)) * (D * (int)sizeof(T));
+            a[i] = *(const Piece<T>*)(src + at0 * (int)sizeof(T));
+            b[i] = *(const Piece<T>*)(src + at1 * (int)sizeof(T));
         }
+        advance(token, head);
     };
-    load(lane / kUnits);
-    if (p.cu_seqlens && t >= p.cu_seqlens[p.n_graphs]) return;
-    const float2 turn = turn_of(p, (int32_t)t);
-    if (lane < D / 2) s_turn[warp][lane] = turn;
-    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) load(i);
+    if (p.cu_seqlens) tokens = (int)min((int64_t)tokens, (int64_t)p.cu_seqlens[p.n_graphs] - t0);
+    if (tokens <= 0) return;
+    if (tid < tokens) s_position[tid] = position_of(p, (int32_t)t0 + tid);
+    __syncthreads();
+    for (int e = tid; e < tokens * (D / 2); e += kThreads) {
+        const int pair = e % (D / 2);
+        if (pair < half) s_turn[e / (D / 2)][pair] = turn_of(p, s_position[e / (D / 2)], p.frequencies[pair]);
+    }
+    __syncthreads();
     if (!mine) return;
-    float2 cs[kVec];
+    while (out_token < tokens) {
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) cs[i] = s_turn[warp][rotated ? unit * kVec + i : 0];
-    for (int h0 = lane / kUnits; h0 < all; h0 += kUnroll * kHeads) {
-        if (h0 != lane / kUnits) load(h0);
+        for (int i = 0; i < kAhead; ++i) {
+            if (out_token < tokens) {
+                if (rotated) {
+                    float2 cs[kVec];
 #pragma unroll
-        for (int i = 0; i < kUnroll; ++i) {
-            const int h = h0 + i * kHeads;
-            if (h >= all) continue;
-            if (rotated) {
-                if (kInterleaved) {
+                    for (int e = 0; e < kVec; e += 2) *(float4*)&cs[e] = *(const float4*)&s_turn[out_token][unit * kVec + e];
 #pragma unroll
                     for (int e = 0; e < kVec; ++e) {
-                        T* pair = e < kVec / 2 ? &a[i].v[2 * e] : &b[i].v[2 * e - kVec];
-                        if (unit * kVec + e < p.rot_dim / 2) {
-                            const float x = widen(pair[0]), y = widen(pair[1]);
-                            pair[0] = narrow<T>(x * cs[e].x - y * cs[e].y);
-                            pair[1] = narrow<T>(x * cs[e].y + y * cs[e].x);
+                        T* x = kInterleaved ? (e < kVec / 2 ? &a[i].v[2 * e] : &b[i].v[2 * e - kVec]) : &a[i].v[e];
+                        T* y = kInterleaved ? x + 1 : &b[i].v[e];
+                        const float u = widen(*x), w = widen(*y);
+                        if (!kInterleaved || unit * kVec + e < half) {
+                            *x = narrow<T>(u * cs[e].x - w * cs[e].y);
+                            *y = narrow<T>(u * cs[e].y + w * cs[e].x);
                         }
                     }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < kVec; ++e) {
-                        const float x = widen(a[i].v[e]), y = widen(b[i].v[e]);
-                        a[i].v[e] = narrow<T>(x * cs[e].x - y * cs[e].y);
-                        b[i].v[e] = narrow<T>(x * cs[e].y + y * cs[e].x);
-                    }
                 }
+                const bool second = out_head >= p.heads[0];
+                uint8_t* dst = (second ? p.y[1] : p.y[0]) + (t0 + out_token) * (second ? p.y_row[1] : p.y_row[0]) +
+                               (out_head - (second ? p.heads[0] : 0)) * (D * (int)sizeof(T));
+                *(Piece<T>*)(dst + at0 * (int)sizeof(T)) = a[i];
+                *(Piece<T>*)(dst + at1 * (int)sizeof(T)) = b[i];
             }
-            int64_t from, to;
-            uint8_t* dst = p.y[where(h, &from, &to)] + to;
-            *(Piece<T>*)(dst + at0 * sizeof(T)) = a[i];
-            *(Piece<T>*)(dst + at1 * sizeof(T)) = b[i];
+            advance(out_token, out_head);
         }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) load(i);
     }
 }
 
@@ -164,15 +161,16 @@ __global__ void __launch_bounds__(kThreads) rotary_any_kernel(const RotaryParams
     grid_wait();
     grid_release();
     const int lane = threadIdx.x & 31;
-    const int64_t t = (int64_t)blockIdx.x * kTokens + (threadIdx.x >> 5);
-    const int32_t end = p.cu_seqlens ? p.cu_seqlens[p.n_graphs] : p.n_total;
+    const int64_t t = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+    const int32_t end = p.cu_seqlens ? min(p.n_total, p.cu_seqlens[p.n_graphs]) : p.n_total;
     if (t >= end) return;
-    const float2 cs = turn_of(p, (int32_t)t);
     const int half = p.rot_dim / 2, i0 = kInterleaved ? 2 * lane : lane, i1 = kInterleaved ? i0 + 1 : i0 + half;
+    const float2 cs = turn_of(p, position_of(p, (int32_t)t), lane < half ? p.frequencies[lane] : 0.0);
     for (int h = 0; h < p.heads[0] + p.heads[1]; ++h) {
-        const int of = h < p.heads[0] ? 0 : 1, head = h - (of ? p.heads[0] : 0);
-        const T* x = (const T*)(p.x[of] + t * p.x_row[of]) + (int64_t)head * D;
-        T* y = (T*)(p.y[of] + t * p.y_row[of]) + (int64_t)head * D;
+        const bool second = h >= p.heads[0];
+        const int head = h - (second ? p.heads[0] : 0);
+        const T* x = (const T*)((second ? p.x[1] : p.x[0]) + t * (second ? p.x_row[1] : p.x_row[0])) + head * D;
+        T* y = (T*)((second ? p.y[1] : p.y[0]) + t * (second ? p.y_row[1] : p.y_row[0])) + head * D;
         if (lane < half) {
             const float a = widen(x[i0]), b = widen(x[i1]);
             y[i0] = narrow<T>(a * cs.x - b * cs.y);
@@ -184,12 +182,21 @@ __global__ void __launch_bounds__(kThreads) rotary_any_kernel(const RotaryParams
 }
 
 template <typename T, int D>
-gt_status launch_rotary(const RotaryParams& p, bool pieces, bool interleaved, cudaStream_t s)
+gt_status launch_rotary(RotaryParams p, bool pieces, bool interleaved, cudaStream_t s)
 {
-    const dim3 grid((unsigned)((p.n_total + kTokens - 1) / kTokens));
-    auto kern = pieces ? (interleaved ? rotary_kernel<T, D, true> : rotary_kernel<T, D, false>)
-                       : (interleaved ? rotary_any_kernel<T, D, true> : rotary_any_kernel<T, D, false>);
-    return launch_overlapped(kern, grid, kThreads, 0, s, p);
+    if (!pieces) {
+        auto kern = interleaved ? rotary_any_kernel<T, D, true> : rotary_any_kernel<T, D, false>;
+        return launch_overlapped(kern, dim3((unsigned)(((int64_t)p.n_total + kThreads / 32 - 1) / (kThreads / 32))), kThreads, 0, s, p);
+    }
+    // Eight pieces per thread, fewer where that leaves less than two blocks per SM.
+    const int all = p.heads[0] + p.heads[1], units = D * (int)sizeof(T) / 32, heads = kThreads / units;
+    int64_t tokens = 8 * heads / all;
+    while (tokens > 1 && (p.n_total + tokens - 1) / tokens < 2 * sm_count()) tokens /= 2;
+    p.tokens = (int32_t)(tokens < 1 ? 1 : tokens > kMaxTokens ? kMaxTokens : tokens);
+    p.step_tokens = heads / all;
+    p.step_heads = heads % all;
+    auto kern = interleaved ? rotary_kernel<T, D, true> : rotary_kernel<T, D, false>;
+    return launch_overlapped(kern, dim3((unsigned)(((int64_t)p.n_total + p.tokens - 1) / p.tokens)), kThreads, 0, s, p);
 }
 
 }  // namespace
