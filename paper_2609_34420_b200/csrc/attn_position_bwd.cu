@@ -575,8 +575,7 @@ struct PrepareParams {
 
 // What the main kernel wants done before it, in one launch.  Row blocks: for every row (t, h), ext[t][h][0..2] = three-term bf16 split of
 // -lse sqrt(d), ext[t][h][8..10] = that of -Delta, Delta = sum_c dO[t,h,c] O[t,h,c], zeros elsewhere; and their share of the accumulators
-// is cleared.  A thread owns a row and adds its products in channel order (a row whose softmax has one key then has dP = Delta to the
-// bit); the rows reach it through shared memory, because 32 lanes that each walk along a row of their own ask the L1 for every line eight
+// is cleared.  A thread owns a row and adds its products in channel order; the rows reach it through shared memory, because 32 lanes that each walk along a row of their own ask the L1 for every line eight
 // times.  16-byte chunk c of row r lies at chunk c ^ (r & 7): eight neighbouring rows' chunks lie in different banks (D = 32: c ^ (r & 3)).
 constexpr int kPrepareThreads = 256, kPrepareRows = 128;
 template <int D>

@@ -302,12 +302,12 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     if constexpr (kSlope) x -= slope2 * fabsf((float)(kv0 + 4 * i - q));
                     if (4 * i < valid) top = fmaxf(top, x);
                 }
-                exact = named_barrier_or(pair_bar, 64, valid > 0 && !(fabsf(top) <= kPeekReach));   // (a half without valid columns has no say)
+                exact = named_barrier_or(pair_bar, 64, valid > 0 && q < n && !(fabsf(top) <= kPeekReach));   // (a half without valid columns has no say)
             }
 
             // Scores of eight consecutive columns in log2 units, plus `add`; `far`: beyond the polynomial's reach.
             float top_u = 0.f;
-            auto scores8 = [&](const uint32_t* sr, int col, float add, auto far, float (&x)[8]) {
+            auto scores8 = [&](const uint32_t* sr, int col, float add, auto rag, auto far, float (&x)[8]) {
                 uint64_t base = both(add);
                 if constexpr (kSlope)
                     if (!mixed) base = both(fmaf(step_slope, (float)(kv0 + col - q), add));
@@ -326,6 +326,10 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         const uint64_t u = mul_f32x2(raw, to_tanh2), uu = mul_f32x2(u, u);
                         float u0, u1;
                         unpack_f32x2(uu, u0, u1);
+                        if constexpr (decltype(rag)::value) {
+                            if (col + i >= valid) u0 = 0.f;
+                            if (col + i + 1 >= valid) u1 = 0.f;
+                        }
                         top_u = fmaxf(top_u, fmaxf(u0, u1));
                         y = fma_f32x2(mul_f32x2(raw, c1c1), tanh_ratio(uu), a);
                     } else {
@@ -348,7 +352,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 #pragma unroll
                         for (int e = 0; e < kCW; e += 8) {
                             float x[8];
-                            scores8(sr + e, c * kCW + e, 0.f, Tag<true>{}, x);
+                            scores8(sr + e, c * kCW + e, 0.f, Tag<false>{}, Tag<true>{}, x);
 #pragma unroll
                             for (int i = 0; i < 8; ++i)
                                 if (c * kCW + e + i < valid) mx = fmaxf(mx, x[i]);
@@ -387,7 +391,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 #pragma unroll
                     for (int e = 0; e < kCW; e += 8) {
                         float x[8];
-                        scores8(sr + e, c * kCW + e, -m, far, x);
+                        scores8(sr + e, c * kCW + e, -m, rag, far, x);
 #pragma unroll
                         for (int i = 0; i < 8; i += 2) {
                             if constexpr (decltype(rag)::value) {
@@ -419,8 +423,9 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 }
                 if (exact) break;
                 // reference too low for some row of this pair of warps?  Also catches inf / NaN, and scores near the cap.
-                const bool beyond = kCap && !wide && !(top_u <= kTanhReach);
-                if (!named_barrier_or(pair_bar, 64, !(tile_sum <= kSumThreshold) || beyond)) break;
+                // (Rows behind the document have no say.)
+                const bool beyond = kCap && !wide && q < n && !(top_u <= kTanhReach);
+                if (!named_barrier_or(pair_bar, 64, (q < n && !(tile_sum <= kSumThreshold)) || beyond)) break;
                 if (kCap && !wide && named_barrier_or(pair_bar, 64, beyond)) wide = true;       // from now on, with the tanh of any score
                 else exact = true;
             }
@@ -452,28 +457,27 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         named_barrier_sync(pair_bar, 64);
         l += xchg[256 + (hf ^ 1) * 128 + r];
         if constexpr (kExact) l_rounded += xchg[(hf ^ 1) * 128 + r];
-        const float inv_l = 1.0f / (kExact ? l_rounded : l);
         uint32_t o[kOC];
         if constexpr (kOC == 32) tmem_ld32(tO, o); else tmem_ld16(tO, o);
         tmem_wait_ld();
         if (q < n) {
-            uint4* dst = (uint4*)(p.out + ((size_t)(node0 + q) * p.n_heads + h) * D + hf * kOC);
-#pragma unroll
-            for (int i = 0; i < kOC / 8; ++i) {
-                uint4 v;
-                v.x = pack_bf16x2(__uint_as_float(o[8 * i]) * inv_l, __uint_as_float(o[8 * i + 1]) * inv_l);
-                v.y = pack_bf16x2(__uint_as_float(o[8 * i + 2]) * inv_l, __uint_as_float(o[8 * i + 3]) * inv_l);
-                v.z = pack_bf16x2(__uint_as_float(o[8 * i + 4]) * inv_l, __uint_as_float(o[8 * i + 5]) * inv_l);
-                v.w = pack_bf16x2(__uint_as_float(o[8 * i + 6]) * inv_l, __uint_as_float(o[8 * i + 7]) * inv_l);
-                dst[i] = v;
-            }
+            float x[kOC];
             if constexpr (kExact) {
+#pragma unroll
+                for (int i = 0; i < kOC; ++i) x[i] = __uint_as_float(o[i]) / l_rounded;      // (a row with one key gets that key's value to the bit)
                 float4* dst32 = (float4*)(p.out_f32 + ((size_t)(node0 + q) * p.n_heads + h) * D + hf * kOC);
 #pragma unroll
-                for (int i = 0; i < kOC / 4; ++i)
-                    dst32[i] = make_float4(__uint_as_float(o[4 * i]) * inv_l, __uint_as_float(o[4 * i + 1]) * inv_l,
-                                           __uint_as_float(o[4 * i + 2]) * inv_l, __uint_as_float(o[4 * i + 3]) * inv_l);
+                for (int i = 0; i < kOC / 4; ++i) dst32[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+            } else {
+                const float inv_l = 1.0f / l;
+#pragma unroll
+                for (int i = 0; i < kOC; ++i) x[i] = __uint_as_float(o[i]) * inv_l;
             }
+            uint4* dst = (uint4*)(p.out + ((size_t)(node0 + q) * p.n_heads + h) * D + hf * kOC);
+#pragma unroll
+            for (int i = 0; i < kOC / 8; ++i)
+                dst[i] = make_uint4(pack_bf16x2(x[8 * i], x[8 * i + 1]), pack_bf16x2(x[8 * i + 2], x[8 * i + 3]), pack_bf16x2(x[8 * i + 4], x[8 * i + 5]),
+                                    pack_bf16x2(x[8 * i + 6], x[8 * i + 7]));
             if (hf == 0) p.lse[(size_t)h * p.n_total + node0 + q] = (m + log2f(l)) * kLn2;
         }
     }

@@ -1,0 +1,299 @@
+"""gt_position_attn_fwd / gt_position_attn_bwd against the fp64 oracle, through the C ABI.
+
+Elementwise, a result may be off by what the oracle derives from half a step of every rounding to bf16; as a whole (2-norm) by what it
+derives from independent roundings, and 10 % for the sample that a result of 4 096 values or more is."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import position_attention as opos
+from paper_2609_34420_b200 import binding as gt
+
+from gpu_util import rel_l2, to_f64
+
+pytestmark = pytest.mark.gpu
+ONE = 2.0 ** -8 / 3 ** 0.5
+WHOLE = ("out", "dq", "dk", "dv")
+LEFT = 77.0          # what lies in results before a call
+
+
+class Case:
+    def __init__(self, lengths, H=4, G=2, d=64, causal=True, prefix=None, slopes=None, cap=0.0, spread=1.0, shift=0.0, extra=0, seed=0, apart=False):
+        rng = np.random.Generator(np.random.PCG64(seed))
+        dev = "cuda"
+        self.cu = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int32)
+        self.n, T = int(self.cu[-1]), int(self.cu[-1]) + extra
+        self.T, self.H, self.G, self.d, self.causal, self.cap = T, H, G, d, causal, cap
+
+        def normal(h, std=1.0):
+            return torch.from_numpy(rng.standard_normal((T, h, d)) * std).bfloat16().to(dev)
+
+        q, k, v, self.dout = normal(H, spread), normal(G), normal(G), normal(H)
+        if shift:                        # every score moves by about `shift`
+            q[:, :, 0], k[:, :, 0] = 8.0, shift
+        if apart:
+            rows = torch.full((T, H + 2 * G + 1, d), LEFT, dtype=torch.bfloat16, device=dev)
+            self.q, self.k, self.v = rows[:, :H], rows[:, H:H + G], rows[:, H + G:H + 2 * G]
+            self.q[:], self.k[:], self.v[:] = q, k, v
+            grads = torch.full_like(rows, LEFT)
+            self.dq, self.dk, self.dv = grads[:, :H], grads[:, H:H + G], grads[:, H + G:H + 2 * G]
+            self.gap = grads[:, H + 2 * G:]
+        else:
+            self.q, self.k, self.v = q, k, v
+            self.dq, self.dk, self.dv = (torch.full_like(x, LEFT) for x in (q, k, v))
+            self.gap = None
+        many = len(lengths) > 1 or extra
+        self.batch = gt.Batch(T, len(lengths), T if len(lengths) == 1 else max(1, *lengths), torch.from_numpy(self.cu).to(dev) if many else None)
+        self.prefix = None if prefix is None else torch.tensor(prefix, dtype=torch.int32, device=dev)
+        self.slopes = None if slopes is None else torch.tensor(slopes, dtype=torch.float32, device=dev)
+        self.out = torch.full((T, H, d), LEFT, dtype=torch.bfloat16, device=dev)
+        self.out32 = torch.full((T, H, d), LEFT, device=dev)
+        self.lse = torch.full((H, T), LEFT, device=dev)
+
+    def forward(self, exact=True, ws=None):
+        return gt.gt_position_attn_fwd(self.q, self.k, self.v, self.slopes, self.prefix, self.batch, self.causal, self.cap, self.out, self.lse,
+                                       self.out32 if exact else None, ws)
+
+    def backward(self, exact=True, ws=None):
+        return gt.gt_position_attn_bwd(self.q, self.k, self.v, self.out, self.dout, self.lse, self.slopes, self.prefix, self.batch, self.causal,
+                                       self.cap, self.dq, self.dk, self.dv, self.out32 if exact else None, ws)
+
+    def oracle(self):
+        n = self.n
+        q, k, v, do = (to_f64(x)[:n] for x in (self.q, self.k, self.v, self.dout))
+        return opos.batch_attention(q, k, v, do, self.cu, self.causal, None if self.prefix is None else self.prefix.tolist(),
+                                    None if self.slopes is None else to_f64(self.slopes), self.cap)
+
+    def results(self):
+        return {"out": to_f64(self.out), "lse": to_f64(self.lse), "dq": to_f64(self.dq), "dk": to_f64(self.dk), "dv": to_f64(self.dv)}
+
+    def check(self, exact=True, ref=None, names=("out", "lse", "dq", "dk", "dv")):
+        ref, got, n = ref or self.oracle(), self.results(), self.n
+        for name in names:
+            x = got[name][:, :n] if name == "lse" else got[name][:n]
+            limit = ref["bounds"][name if exact or name not in ("dq", "dk") else name + "_out"]
+            off = np.abs(x - ref[name])
+            assert np.all(off <= limit), (name, float((off / limit).max()), np.argwhere(~(off <= limit))[:4].tolist())
+            if name in WHOLE and (exact or name not in ("dq", "dk")) and x.size >= 4096:
+                assert np.linalg.norm(x - ref[name]) <= 1.1 * ref["norms"][name], (name, float(np.linalg.norm(x - ref[name]) / ref["norms"][name]))
+            behind = got[name][:, n:] if name == "lse" else got[name][n:]
+            assert np.all(behind == LEFT), name
+        assert self.gap is None or bool((self.gap == LEFT).all())
+        return ref
+
+    def run(self, exact=True):
+        self.forward_ws = self.forward(exact)
+        gt.gt_check(self.forward_ws)
+        gt.gt_check(self.backward(exact))
+        return self.check(exact)
+
+
+@pytest.mark.parametrize("n", [1, 2, 3, 31, 32, 33, 63, 64, 65, 127, 128, 129, 191, 255, 256, 257, 300, 384, 385, 513])
+@pytest.mark.parametrize("d", [32, 64])
+@pytest.mark.parametrize("causal", [True, False])
+def test_lengths(n, d, causal):
+    Case([n], H=2, G=1, d=d, causal=causal, seed=n).run()
+
+
+@pytest.mark.parametrize("H,G", [(1, 1), (3, 3), (4, 1), (6, 2), (8, 4), (12, 4)])
+def test_heads(H, G):
+    Case([200], H=H, G=G, seed=H).run()
+
+
+OPTIONS = [dict(), dict(cap=5.0, spread=3.0), dict(slopes=True), dict(prefix=True), dict(prefix=True, slopes=True, cap=20.0, spread=6.0),
+           dict(causal=False, slopes=True), dict(causal=False, cap=2.0, spread=4.0), dict(causal=False, slopes=True, cap=50.0, spread=2.0),
+           dict(spread=15.0), dict(spread=15.0, slopes=True), dict(cap=30.0, spread=25.0), dict(shift=30.0), dict(shift=-30.0),
+           dict(shift=-30.0, causal=False, slopes=True), dict(cap=50.0, shift=-30.0), dict(cap=1e-3), dict(cap=1e6)]
+
+
+@pytest.mark.parametrize("options", OPTIONS)
+@pytest.mark.parametrize("lengths", [[600], [1, 130, 0, 300, 5, 0, 256, 128, 7], [0, 0, 129, 384, 0]])
+@pytest.mark.parametrize("d", [32, 64])
+def test_options(options, lengths, d):
+    o = dict(options)
+    if o.pop("slopes", False):
+        o["slopes"] = [0.5, 0.0625, 0.0, 2.0]
+    if o.pop("prefix", False):
+        o["prefix"] = [[9, 200, -5, 1 << 30, 3, 0, 129, 128, -(1 << 31)][i % 9] for i in range(len(lengths))]
+    Case(lengths, d=d, seed=len(lengths), **o).run()
+
+
+@pytest.mark.parametrize("prefix", [1, 64, 127, 128, 129, 255, 256, 257, 299, 300, 301])
+def test_prefixes_at_the_edges_of_tiles(prefix):
+    Case([300], H=2, G=2, prefix=[prefix], slopes=[0.1, 1.0], seed=prefix).run()
+    Case([700, 300, 520], H=2, G=2, prefix=[prefix] * 3, seed=prefix).run()
+
+
+@pytest.mark.parametrize("exact", [True, False])
+def test_rows_apart_and_rows_behind_the_last_document(exact):
+    Case([100, 0, 257, 60], H=4, G=2, cap=10.0, spread=2.0, extra=150, apart=True, seed=1).run(exact)
+    Case([300], H=4, G=4, extra=1, apart=True, seed=2).run(exact)
+    empty = Case([0, 0], H=2, G=1, extra=3)
+    gt.gt_check(empty.forward(exact))
+    gt.gt_check(empty.backward(exact))
+    assert all((x == LEFT).all() for x in empty.results().values())
+
+
+def test_without_the_fp32_output_peaked_rows_stay_within_their_bounds():
+    Case([400, 33], H=4, G=4, spread=6.0, seed=5).run(exact=False)
+
+
+def test_large_blocks_of_two_tiles_and_the_work_list():
+    """Enough documents for blocks of two query tiles and, in the backward, the list of the work."""
+    rng = np.random.Generator(np.random.PCG64(3))
+    Case([int(n) for n in rng.integers(0, 700, 24)], H=8, G=2, prefix=[int(n) for n in rng.integers(0, 300, 24)], slopes=list(2.0 ** -np.arange(1, 9)),
+         cap=30.0, spread=3.0, seed=4).run()
+    Case([int(n) for n in rng.integers(1, 90, 70)] + [1000], H=8, G=8, seed=6).run()
+
+
+def test_many_documents_of_very_different_lengths():
+    lengths = [1200] + [5] * 300
+    Case(lengths, H=4, G=4, d=32, seed=8).run()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_other_documents_values_do_not_leak(causal):
+    """NaN and infinities in the rows of another document, and behind the last one, change nothing."""
+    kw = dict(lengths=[70, 200, 300], H=4, G=2, causal=causal, extra=40, seed=11)
+    clean = Case(**kw)
+    clean.run()
+    for bad in (float("nan"), float("inf")):
+        c = Case(**kw)
+        for x in (c.q, c.k, c.v, c.dout):
+            x[70:270] = bad
+            x[570:] = -bad
+        gt.gt_check(c.forward())
+        c.lse[:, 70:270] = bad
+        c.out32[70:270] = bad
+        gt.gt_check(c.backward())
+        for rows in (slice(0, 70), slice(270, 570)):
+            assert torch.equal(c.out[rows], clean.out[rows]) and torch.equal(c.lse[:, rows], clean.lse[:, rows])
+            for name in ("dq", "dk", "dv"):
+                x, y = to_f64(getattr(c, name)[rows]), to_f64(getattr(clean, name)[rows])
+                assert np.isfinite(x).all() and rel_l2(x, y) <= 2 * ONE, name              # (the order of the sums)
+        assert bool((c.out[570:] == LEFT).all()) and bool((c.dk[570:] == LEFT).all())
+
+
+def test_keys_that_no_query_may_see_yet_do_not_matter():
+    """Large finite values in the future of a causal row stay without effect."""
+    c = Case([256], H=2, G=2, seed=12)
+    c.run()
+    ref = to_f64(c.out)[:128]
+    c.k[128:], c.v[128:] = 300.0, -300.0
+    gt.gt_check(c.forward())
+    assert np.array_equal(to_f64(c.out)[:128], ref)
+
+
+def test_another_stream():
+    c = Case([500, 300], H=4, G=2, seed=13)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        a, b = c.forward(), c.backward()
+        gt.gt_check(a)
+        gt.gt_check(b)
+    c.check()
+
+
+def test_captured_and_replayed():
+    c = Case([400, 300], H=4, G=2, prefix=[10, 200], seed=14)
+    wf, wb = c.forward(), c.backward()
+    gt.gt_check(wb)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        c.forward(ws=wf)
+        c.backward(ws=wb)
+    other = Case([400, 300], H=4, G=2, prefix=[10, 200], seed=15)
+    for x in ("q", "k", "v", "dout"):
+        getattr(c, x).copy_(getattr(other, x))
+    for _ in range(2):
+        for x in (c.out, c.out32, c.lse, c.dq, c.dk, c.dv):
+            x.fill_(LEFT)
+        g.replay()
+        gt.gt_check(wf)
+        gt.gt_check(wb)
+        c.check()
+
+
+def test_the_same_call_twice_and_one_workspace_for_both_directions():
+    c = Case([333, 64, 1], H=4, G=1, slopes=[0.1] * 4, seed=16)
+    size = max(gt.gt_position_attn_fwd_workspace(c.batch, 4, 1, 64), gt.gt_position_attn_bwd_workspace(c.batch, 4, 1, 64))
+    ws = gt._workspace(size, "cuda")
+    ref = None
+    for _ in range(3):
+        c.forward(ws=ws)
+        c.backward(ws=ws)
+        gt.gt_check(ws)
+        ref = c.check(ref=ref)
+
+
+def test_forward_is_the_same_from_run_to_run():
+    c = Case([777], H=8, G=8, cap=10.0, seed=17)
+    c.forward()
+    first = c.out.clone(), c.lse.clone(), c.out32.clone()
+    c.forward()
+    assert all(torch.equal(a, b) for a, b in zip(first, (c.out, c.lse, c.out32)))
+
+
+def test_fp32_output():
+    c = Case([300, 20], H=4, G=2, spread=4.0, seed=18)
+    ref = c.run()
+    off = np.abs(to_f64(c.out32)[:320] - ref["out"])
+    assert np.all(off <= ref["bounds"]["out"])
+    assert np.linalg.norm(to_f64(c.out32) - ref["out"]) <= 1.1 * ref["norms"]["out"]
+    assert torch.equal(c.out32.bfloat16(), c.out)
+
+
+def test_one_key_gives_exactly_its_value():
+    c = Case([1, 1, 1], H=4, G=4, seed=19)
+    c.run()
+    assert torch.equal(c.out, c.v) and torch.equal(c.out32, c.v.float()) and torch.equal(c.dv, c.dout)
+
+
+def test_offsets_beyond_32_bits():
+    """q and out of more than 2^31 elements; the last documents."""
+    n, docs, H, d = 40, 13200, 64, 64
+    T = n * docs
+    assert T * H * d > 1 << 31
+    q = torch.zeros(T, H, d, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    last = slice(T - 3 * n, T)
+    q[last] = torch.randn(3 * n, H, d, device="cuda", generator=g).bfloat16()
+    k, v = (torch.randn(T, 1, d, device="cuda", generator=g).bfloat16() for _ in range(2))
+    cu = torch.arange(docs + 1, device="cuda", dtype=torch.int32) * n
+    out, lse = torch.empty_like(q), torch.empty(H, T, device="cuda")
+    batch = gt.Batch(T, docs, n, cu)
+    ws = gt.gt_position_attn_fwd(q, k, v, None, None, batch, True, 0.0, out, lse)
+    gt.gt_check(ws)
+    ref = opos.batch_attention(to_f64(q[last]), to_f64(k[last]), to_f64(v[last]), None, np.arange(4) * n, True)
+    assert np.all(np.abs(to_f64(out[last]) - ref["out"]) <= ref["bounds"]["out"])
+    assert np.all(np.abs(to_f64(lse[:, last]) - ref["lse"]) <= ref["bounds"]["lse"])
+    dout = torch.zeros_like(q)
+    dout[last] = torch.randn(3 * n, H, d, device="cuda", generator=g).bfloat16()
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    gt.gt_check(gt.gt_position_attn_bwd(q, k, v, out, dout, lse, None, None, batch, True, 0.0, dq, dk, dv))
+    ref = opos.batch_attention(to_f64(q[last]), to_f64(k[last]), to_f64(v[last]), to_f64(dout[last]), np.arange(4) * n, True)
+    for name, x in (("dq", dq), ("dk", dk), ("dv", dv)):
+        off = "" if name == "dv" else "_out"
+        assert np.all(np.abs(to_f64(x[last]) - ref[name]) <= ref["bounds"][name + off]), name
+    assert not dq[:last.start].any() and not dv[:last.start].any()
+
+
+def test_layer_with_rotary_positions():
+    """Rotation, attention and their gradients in a row, as a layer uses them, against the oracle of the whole."""
+    lengths, H, G, d, rot = [300, 1, 150], 4, 2, 64, 32
+    c = Case(lengths, H=H, G=G, d=d, cap=20.0, spread=2.0, seed=20)
+    f = gt.gt_rotary_frequencies(rot, 10000.0, "parts", 4.0, 100, 1.0, 8.0)
+    fd = f.cuda()
+    q0, k0 = c.q.clone(), c.k.clone()
+    gt.gt_rotary(c.q, c.k, fd, None, c.batch, False, 1.1, False, c.q, c.k)              # in place
+    ref = c.run()
+    position = np.concatenate([np.arange(n) for n in lengths])
+    for x, x0 in ((c.q, q0), (c.k, k0)):
+        y = opos.rotate(to_f64(x0), f.numpy(), position, False, 1.1)
+        assert np.all(np.abs(to_f64(x) - y) <= 2.0 ** -8 * np.abs(y) + 1e-6 * np.abs(to_f64(x0)).max())
+    dq, dk = torch.empty_like(c.dq), torch.empty_like(c.dk)
+    gt.gt_rotary(c.dq, c.dk, fd, None, c.batch, False, 1.1, True, dq, dk)
+    for name, x in (("dq", dq), ("dk", dk)):
+        y = opos.rotate(ref[name], f.numpy(), position, False, 1.1, True)
+        assert np.linalg.norm(to_f64(x) - y) <= 1.1 * 1.1 * ref["norms"][name] + ONE * np.linalg.norm(y), name          # (turned and scaled by 1.1, rounded once more)
