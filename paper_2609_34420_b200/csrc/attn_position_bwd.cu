@@ -372,7 +372,7 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 
             // ---------------- P^T = exp2((S^T - lse sqrt(d)) c1), or exp2(cap log2(e) tanh(S^T / cap) - lse log2(e)) ----------------
             float top_u = 0.f;
-            auto probabilities = [&](auto wide) {
+            auto probabilities = [&](auto masked_, auto general) {        // general: any score, any distance
                 uint32_t sv[32];
                 tmem_ld32(tS, sv);
                 tmem_wait_ld();
@@ -384,14 +384,14 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         add = pack_f32x2(nl.x, nl.y);
                     }
                     if constexpr (kSlope) {
-                        if (mixed) add = add_f32x2(add, pack_f32x2(-slope2 * fabsf((float)(q0 + c - key)), -slope2 * fabsf((float)(q0 + c + 1 - key))));
+                        if constexpr (decltype(general)::value) add = add_f32x2(add, pack_f32x2(-slope2 * fabsf((float)(q0 + c - key)), -slope2 * fabsf((float)(q0 + c + 1 - key))));
                         else add = fma_f32x2(both(step_slope), pack_f32x2((float)(q0 + c - key), (float)(q0 + c + 1 - key)), add);
                     }
                     const uint64_t raw = pack_u32x2(sv[c], sv[c + 1]);
                     [[maybe_unused]] uint64_t t;
                     if constexpr (kCap) {
                         const uint64_t u = mul_f32x2(raw, to_tanh2);
-                        if constexpr (decltype(wide)::value) {
+                        if constexpr (decltype(general)::value) {
                             float u0, u1;
                             unpack_f32x2(u, u0, u1);
                             t = pack_f32x2(tanh_any(u0), tanh_any(u1));
@@ -412,7 +412,7 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     unpack_f32x2(x, lo, hi);
                     lo = ex2_approx(lo);
                     hi = ex2_approx(hi);
-                    if (masked) {
+                    if constexpr (decltype(masked_)::value) {
                         if (c < c_from || c >= c_to) lo = 0.f;
                         if (c + 1 < c_from || c + 1 >= c_to) hi = 0.f;
                     }
@@ -426,9 +426,13 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     }
                 }
             };
-            probabilities(Tag<false>{});
-            if constexpr (kCap)
-                if (__any_sync(0xffffffffu, !(top_u <= kTanhReach))) probabilities(Tag<true>{});
+            if (mixed) probabilities(Tag<true>{}, Tag<true>{});
+            else {
+                if (masked) probabilities(Tag<true>{}, Tag<false>{});
+                else probabilities(Tag<false>{}, Tag<false>{});
+                if constexpr (kCap)
+                    if (__any_sync(0xffffffffu, !(top_u <= kTanhReach))) probabilities(Tag<true>{}, Tag<true>{});
+            }
             tmem_st16(tS, pk);                      // P^T of this group: 16 packed columns at the start of its range
             uint32_t dpa[16], dpb[16];
             mbar_wait(bar(kBarDpFull + half), i & 1, abort_flag, p.status, 341);
@@ -442,21 +446,26 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             tmem_wait_ld();
 
             // ---------------- dS^T = P^T o (dP^T - Delta) ----------------
-            auto ds_round = [&](int rnd, const uint32_t (&dp)[16]) {
+            auto ds_round = [&](int rnd, const uint32_t (&dp)[16], auto masked_) {
 #pragma unroll
                 for (int k = 0; k < 16; k += 2) {
                     const int c = rnd * 16 + k;
                     float lo, hi;
                     unpack_f32x2(mul_f32x2(pack_f32x2(pr[c], pr[c + 1]), pack_u32x2(dp[k], dp[k + 1])), lo, hi);
-                    if (masked) {                    // (0 x NaN: a row of V that is another document's, or of this one's queries that do not see the key)
+                    if constexpr (decltype(masked_)::value) {      // (0 x NaN: a row of V that is another document's, or of this one's queries that do not see the key)
                         if (c < c_from || c >= c_to) lo = 0.f;
                         if (c + 1 < c_from || c + 1 >= c_to) hi = 0.f;
                     }
                     pk[c >> 1] = pack_bf16x2(lo, hi);
                 }
             };
-            ds_round(0, dpa);
-            ds_round(1, dpb);
+            if (masked) {
+                ds_round(0, dpa, Tag<true>{});
+                ds_round(1, dpb, Tag<true>{});
+            } else {
+                ds_round(0, dpa, Tag<false>{});
+                ds_round(1, dpb, Tag<false>{});
+            }
             tmem_st16(tDp, pk);
             // dQ of the previous tile has read the dS^T tile in shared memory
             if (i > 0) mbar_wait(bar(kBarDqFull), (i - 1) & 1, abort_flag, p.status, 342);

@@ -305,19 +305,19 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 exact = named_barrier_or(pair_bar, 64, valid > 0 && q < n && !(fabsf(top) <= kPeekReach));   // (a half without valid columns has no say)
             }
 
-            // Scores of eight consecutive columns in log2 units, plus `add`; `far`: beyond the polynomial's reach.
+            // Scores of eight consecutive columns in log2 units, plus `add`; general: any score, any distance.
             float top_u = 0.f;
-            auto scores8 = [&](const uint32_t* sr, int col, float add, auto rag, auto far, float (&x)[8]) {
+            auto scores8 = [&](const uint32_t* sr, int col, float add, auto rag, auto general, float (&x)[8]) {
                 uint64_t base = both(add);
                 if constexpr (kSlope)
-                    if (!mixed) base = both(fmaf(step_slope, (float)(kv0 + col - q), add));
+                    if constexpr (!decltype(general)::value) base = both(fmaf(step_slope, (float)(kv0 + col - q), add));
 #pragma unroll
                 for (int i = 0; i < 8; i += 2) {
                     const uint64_t raw = pack_u32x2(sr[i], sr[i + 1]);
                     uint64_t a = base, y;
                     if constexpr (kSlope)
-                        if (!mixed) a = add_f32x2(base, pack_f32x2(step_slope * (float)i, step_slope * (float)(i + 1)));
-                    if constexpr (kCap && decltype(far)::value) {
+                        if constexpr (!decltype(general)::value) a = add_f32x2(base, pack_f32x2(step_slope * (float)i, step_slope * (float)(i + 1)));
+                    if constexpr (kCap && decltype(general)::value) {
                         float u0, u1, a0, a1;
                         unpack_f32x2(mul_f32x2(raw, to_tanh2), u0, u1);
                         unpack_f32x2(a, a0, a1);
@@ -337,7 +337,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     }
                     unpack_f32x2(y, x[i], x[i + 1]);
                     if constexpr (kSlope)
-                        if (mixed) {
+                        if constexpr (decltype(general)::value) {
                             x[i] = fmaf(-slope2, fabsf((float)(kv0 + col + i - q)), x[i]);
                             x[i + 1] = fmaf(-slope2, fabsf((float)(kv0 + col + i + 1 - q)), x[i + 1]);
                         }
@@ -387,11 +387,11 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 // ---- P = 2^(score - m), row sum ----
                 uint64_t sum2 = pack_f32x2(0.f, 0.f);
                 rounded2 = sum2;
-                auto exp_chunk = [&](int c, const uint32_t (&sr)[kCW], auto rag, auto far) {
+                auto exp_chunk = [&](int c, const uint32_t (&sr)[kCW], auto rag, auto general) {
 #pragma unroll
                     for (int e = 0; e < kCW; e += 8) {
                         float x[8];
-                        scores8(sr + e, c * kCW + e, -m, rag, far, x);
+                        scores8(sr + e, c * kCW + e, -m, rag, general, x);
 #pragma unroll
                         for (int i = 0; i < 8; i += 2) {
                             if constexpr (decltype(rag)::value) {
@@ -405,14 +405,14 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         }
                     }
                 };
-                auto exp_pass = [&](auto rag, auto far) {
+                auto exp_pass = [&](auto rag, auto general) {
                     if (!loaded) load_chunk(0, sa);
-                    tmem_wait_ld(); load_chunk(1, sb); exp_chunk(0, sa, rag, far);
-                    tmem_wait_ld(); load_chunk(2, sa); exp_chunk(1, sb, rag, far);
-                    tmem_wait_ld(); load_chunk(3, sb); exp_chunk(2, sa, rag, far);
-                    tmem_wait_ld(); exp_chunk(3, sb, rag, far);
+                    tmem_wait_ld(); load_chunk(1, sb); exp_chunk(0, sa, rag, general);
+                    tmem_wait_ld(); load_chunk(2, sa); exp_chunk(1, sb, rag, general);
+                    tmem_wait_ld(); load_chunk(3, sb); exp_chunk(2, sa, rag, general);
+                    tmem_wait_ld(); exp_chunk(3, sb, rag, general);
                 };
-                if (kCap && (exact || wide)) exp_pass(Tag<true>{}, Tag<kCap>{});
+                if (mixed || (kCap && (exact || wide))) exp_pass(Tag<true>{}, Tag<kCap || kSlope>{});
                 else if (ragged) exp_pass(Tag<true>{}, Tag<false>{});
                 else exp_pass(Tag<false>{}, Tag<false>{});
                 loaded = false;
