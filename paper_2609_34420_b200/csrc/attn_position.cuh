@@ -44,8 +44,43 @@ __device__ __forceinline__ float tanh_any(float y)
     return u <= kTanhReach ? p : fmaf(-2.0f, r, 1.0f);
 }
 
+// Words of the workspace's header that no other call uses: counters of the persistent kernels, 0 between calls.
+constexpr int kNextForward = 16, kNextBackward = 17;
+
 // A query at position i of a document of n tokens sees the document's keys [0, row_limit).
 __device__ __forceinline__ int32_t row_limit(bool causal, int32_t i, int32_t prefix, int32_t n) { return causal ? min(n, max(i + 1, prefix)) : n; }
+
+// Work list of a packed batch (write_work_list) in which, with causal documents, the blocks with the most keys (in the backward: queries)
+// come first, whatever their document: block j of a document of b blocks has work b - j.
+template <int kRows>
+__device__ __forceinline__ void write_list(int4* list, int32_t entries, const int32_t* __restrict__ cu_seqlens, int32_t n_graphs, int32_t g, bool causal)
+{
+    if (!causal || n_graphs > kListSorted) {
+        write_work_list<kRows>(list, entries, cu_seqlens, n_graphs, g);
+        return;
+    }
+    const int lane = threadIdx.x & 31;
+    const int32_t c0 = cu_seqlens[g], n = cu_seqlens[g + 1] - c0, blocks = (n + kRows - 1) / kRows;
+    int32_t other[kListSorted / 32];                       // a lane's documents' blocks
+    int32_t all = 0;
+#pragma unroll
+    for (int i = 0; i < kListSorted / 32; ++i) {
+        const int j = lane + 32 * i;
+        other[i] = j < n_graphs ? (cu_seqlens[j + 1] - cu_seqlens[j] + kRows - 1) / kRows : 0;
+        all += other[i];
+    }
+    all = __reduce_add_sync(0xffffffffu, all);
+    for (int32_t block = 0; block < blocks; ++block) {
+        const int32_t work = blocks - block;
+        int32_t before = 0;                                // entries with more work, and with as much of a document before this one
+#pragma unroll
+        for (int i = 0; i < kListSorted / 32; ++i) before += max(0, other[i] - work) + (lane + 32 * i < g && other[i] >= work ? 1 : 0);
+        before = __reduce_add_sync(0xffffffffu, before);
+        if (lane == 0) list[before] = make_int4(g, block, c0, n);
+    }
+    if (g == 0)
+        for (int32_t i = all + lane; i < entries; i += 32) list[i] = make_int4(-1, 0, 0, 0);
+}
 
 // go(Tag<wide>, Tag<capped>, Tag<sloped>) for three values that are known when the program runs.
 template <typename Go>

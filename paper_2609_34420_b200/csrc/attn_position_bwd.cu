@@ -97,6 +97,7 @@ struct Smem {
     static constexpr int kBars = kLse + kSoftmaxWarps * 128;
     static constexpr int kMisc = kBars + kNumBarriers * 8;
     static constexpr int kDynamic = kMisc + 16 + 1024;              // slack for the 1024-byte alignment
+    static_assert(kOnes % 1024 == 0 && kQ % 1024 == 0 && kExt % 1024 == 0 && kStg % 1024 == 0 && kDs % 1024 == 0 && kLse % 16 == 0 && kBars % 8 == 0, "aligned");
 };
 
 // register budget: the CTA is launched with 768 x 80 registers; after the re-split it holds

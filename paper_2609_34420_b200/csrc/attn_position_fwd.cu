@@ -2,17 +2,20 @@
 //     out_i = sum_j softmax_j(S_i)_j v_j,   S_ij = cap tanh(q_i . k_j / (sqrt(d) cap)) - slopes[h] |i - j|,
 // over the keys that the document, the causal order and the prefix leave a query.  Positions are indices, so nothing but q, k and v is read.
 //
-// One CTA = one head x 256 query rows (two 128-row tiles, so that the tensor pipe works on one while the other is in its softmax) x the
-// key tiles that any of its rows sees.
+// The grid is persistent: a CTA takes one item of work (a head and one or two 128-row query tiles of a document) after the other, and its
+// warps run through them as through one long row of key tiles.  The next item's rows are fetched, and its first scores made, while the
+// last one's outputs are still written; with a CTA per item, 64 causal documents of 512-2 048 tokens spent 40 % of the time on filling and
+// draining (551 -> @@ us).
 //
-//   warp 0      TMA producer: Q once; K and V through 2-stage rings
+//   warp 0      TMA producer: Q (two items' worth) and K, V through 2-stage rings
 //   warp 1      issues S_t = Q_t K^T for both query tiles
+//   warp 2      fetches the items, two ahead
 //   warp 3      issues O_t += P_t V (A from TMEM, B = V as MN-major); clears what lies behind the document in its last V tile
 //   warps 4-19  softmax: 8 warps per query tile, 4 per half of the 128 key columns (thread = query row = TMEM lane, 64 scores)
 //
 // The key tiles come from the diagonal down to the document's beginning, then the ones behind the diagonal: with a penalty on distance
-// the scores fall along that way, so that a row's reference stays in reach.  A causal block of two tiles begins with a key tile that
-// only the second one sees; the first one skips that step.
+// the scores fall along that way, so that a row's reference stays in reach.  A causal item of two tiles begins with a key tile that only
+// the second one sees; the first one skips that step.  Where a document has an odd number of tiles, its first one is an item of its own.
 //
 // Softmax: a tile is exponentiated against the row's reference at once (0 at first), without a look at its maximum; the tile's row sum
 // tells whether the reference was out of reach, and only then it is redone with the maximum first.  References are whole numbers in log2
@@ -21,6 +24,8 @@
 // TMEM columns: three score buffers [0,128) [128,256) [256,384), used in turn by the steps (key tile, query tile), so that the S MMA of
 // a step never waits for a softmax; P overwrites the part of a buffer that its own thread has read; O_0 [384,448), O_1 [448,512).
 #include <math.h>
+
+#include <algorithm>
 
 #include "attn_position.cuh"
 
@@ -45,7 +50,10 @@ struct PositionFwdParams {
     float* out_f32;            // [T,H,D] fp32, or nullptr
     float* lse;                // [H,T]
     uint32_t* status;
-    const int4* list;          // packed batch: work list; block index = entry * heads + head (nullptr: grid of heads x blocks x documents)
+    uint32_t* next_item;       // counts the items that have been taken beyond the grid's first ones; 0 before and after the kernel
+    const int4* list;          // packed batch: work list; item = entry * heads + head (nullptr: heads, then documents, then blocks)
+    int32_t n_items;
+    int32_t n_graphs;
     int32_t n_total;
     int32_t n_heads;
     int32_t group;             // query heads per key head
@@ -57,14 +65,18 @@ struct PositionFwdParams {
 };
 
 enum Barrier {
-    kBarQFull = 0,
-    kBarKFull = 1,                        // [kStages]
+    kBarItemFull = 0,                     // [2]  an item's description
+    kBarItemEmpty = kBarItemFull + 2,     // [2]  all warps that work on it have read it
+    kBarFetch = kBarItemEmpty + 2,        //      the next item is soon wanted
+    kBarQFull = kBarFetch + 1,            // [2]
+    kBarQEmpty = kBarQFull + 2,           // [2]  commit behind the item's last S MMAs
+    kBarKFull = kBarQEmpty + 2,           // [kStages]
     kBarKEmpty = kBarKFull + kStages,     // [kStages]  commit behind the S MMAs of the key tile
     kBarVFull = kBarKEmpty + kStages,     // [kStages]
     kBarVEmpty = kBarVFull + kStages,     // [kStages]  commit behind the PV MMAs of the key tile
-    kBarSFull = kBarVEmpty + kStages,     // [3]  per score buffer
-    kBarBufFree = kBarSFull + 3,          // [3]  P of the buffer consumed by its PV MMA
-    kBarPFull = kBarBufFree + 3,          // [2 tiles][2 parities of the tile's steps]
+    kBarBufFree = kBarVEmpty + kStages,   // [3]  per score buffer: P consumed by its PV MMA
+    kBarSFull = kBarBufFree + 3,          // [2 tiles][2 parities of the tile's steps]
+    kBarPFull = kBarSFull + 4,            // [2 tiles][2 parities]
     kBarODone = kBarPFull + 4,            // [2 tiles][2 parities]
     kNumBarriers = kBarODone + 4
 };
@@ -74,15 +86,44 @@ struct Smem {
     static constexpr int kRowBytes = D * 2;
     static constexpr int kTileBytes = 128 * kRowBytes;
     static constexpr int kQ = 0;
-    static constexpr int kK = kQ + 2 * kTileBytes;
+    static constexpr int kK = kQ + 4 * kTileBytes;               // Q: [2 items][2 tiles]
     static constexpr int kV = kK + kStages * kTileBytes;
     static constexpr int kXchg = kV + kStages * kTileBytes;      // [2 tiles][max | sum][2 halves][128 rows] float
     static constexpr int kBars = kXchg + 2 * 512 * 4;
-    static constexpr int kMisc = kBars + kNumBarriers * 8;
+    static constexpr int kItems = (kBars + kNumBarriers * 8 + 15) / 16 * 16;      // [2] Item
+    static constexpr int kMisc = kItems + 2 * 32;
     static constexpr int kDynamic = kMisc + 16 + 1024;           // slack for the 1024-byte alignment
+    static_assert(kXchg % 16 == 0 && kBars % 8 == 0 && kItems % 16 == 0 && kMisc % 16 == 0 && kDynamic <= 227 * 1024, "aligned, and within an SM");
+};
+
+struct alignas(16) Item {
+    int32_t node0, n, head, q_block;       // n = 0: there are no more
+    int32_t prefix, pad[3];
+};
+
+// What follows from an item: its query tiles and the key tiles that they see.
+struct Span {
+    int32_t q0, tiles, diagonal, n_kv, skip;
+    // kTiles query tiles per block, counted from the document's end
+    template <int kTiles>
+    __device__ __forceinline__ void set(const Item& item, bool causal)
+    {
+        const int32_t n_tiles = (item.n + kTile - 1) / kTile, odd = kTiles == 2 ? n_tiles & 1 : 0, first = max(0, item.q_block * kTiles - odd);
+        tiles = kTiles == 2 && odd && item.q_block == 0 ? 1 : kTiles;
+        q0 = first * kTile;
+        diagonal = first + tiles - 1;
+        n_kv = causal ? max(diagonal + 1, (min(item.n, item.prefix) + kTile - 1) / kTile) : n_tiles;
+        // key tiles that the first query tile does not see: the item's first one, or none
+        skip = tiles == 2 && causal && item.prefix <= diagonal * kTile ? 1 : 0;
+    }
+    __device__ __forceinline__ int32_t key_tile(int32_t s) const { return s <= diagonal ? diagonal - s : s; }
+    __device__ __forceinline__ int32_t steps() const { return tiles * n_kv - skip; }
 };
 
 constexpr int kNbPair = 2;                    // named barriers: + 4 t + lane quarter, the two warps that share 32 query rows
+
+// register budget with two tiles: the CTA is launched with 640 x 96 registers and shares out 128 x 56 + 512 x 104 = 60416 <= 61440
+__device__ __forceinline__ void setmaxnreg_dec_56() { asm volatile("setmaxnreg.dec.sync.aligned.u32 56;"); }
 
 // kTiles = 1: blocks of one query tile, for grids that would leave half of the SMs idle or more.
 // kExact (with the fp32 output): O is divided by the sum of the probabilities as the MMA reads them, rounded to bf16, so that their
@@ -95,152 +136,231 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     const __grid_constant__ CUtensorMap tmap_v, const PositionFwdParams p)
 {
     using L = Smem<D>;
-    constexpr int kRows = kTile * kTiles, kBuffers = kTiles + 1;
+    constexpr int kBuffers = kTiles + 1, kReaders = 3 + 8 * kTiles;          // kReaders: warps that work on an item
     constexpr uint32_t kOCol = 384;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    int h = blockIdx.x, g = blockIdx.z;
-    if (p.cu_seqlens) grid_wait();          // a single document's blocks set up their barriers and tensor memory before they wait
-    int32_t node0 = 0, n = p.n_total, q_block = blockIdx.y;
-    if (p.list) {
-        const int4 entry = p.list[blockIdx.x / (unsigned)p.n_heads];
-        if (entry.x < 0) return;
-        h = (int)(blockIdx.x % (unsigned)p.n_heads);
-        g = entry.x;
-        q_block = entry.y;
-        node0 = entry.z;
-        n = entry.w;
-    } else if (p.cu_seqlens) {
-        node0 = p.cu_seqlens[g];
-        n = p.cu_seqlens[g + 1] - node0;
-    }
-    if (q_block * kRows >= n) return;
-    if (p.causal) q_block = (n - 1) / kRows - q_block;               // the blocks with the most keys first
-    const int32_t q0 = q_block * kRows, n_tiles = (n + kTile - 1) / kTile;
     uint64_t* bars = (uint64_t*)(smem + L::kBars);
     uint32_t* misc = (uint32_t*)(smem + L::kMisc);       // [0] TMEM base, [1] abort flag
+    Item* items = (Item*)(smem + L::kItems);
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     volatile uint32_t* abort_flag = &misc[1];
     if (tid == 0) {
         misc[1] = 0u;
-        mbar_init(bar(kBarQFull), 1);
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(bar(kBarItemFull + s), 1);
+            mbar_init(bar(kBarItemEmpty + s), kReaders);
+            mbar_init(bar(kBarQFull + s), 1);
+            mbar_init(bar(kBarQEmpty + s), 1);
+        }
+        mbar_init(bar(kBarFetch), 1);
         for (int s = 0; s < kStages; ++s) {
             mbar_init(bar(kBarKFull + s), 1);
             mbar_init(bar(kBarKEmpty + s), 1);
             mbar_init(bar(kBarVFull + s), 1);
             mbar_init(bar(kBarVEmpty + s), 1);
         }
-        for (int b = 0; b < 3; ++b) { mbar_init(bar(kBarSFull + b), 1); mbar_init(bar(kBarBufFree + b), 1); }
-        for (int t = 0; t < 4; ++t) { mbar_init(bar(kBarPFull + t), 8); mbar_init(bar(kBarODone + t), 1); }       // (P: one arrival per warp)
+        for (int b = 0; b < 3; ++b) mbar_init(bar(kBarBufFree + b), 1);
+        for (int t = 0; t < 4; ++t) {
+            mbar_init(bar(kBarSFull + t), 1);
+            mbar_init(bar(kBarPFull + t), 8);                // one arrival per warp
+            mbar_init(bar(kBarODone + t), 1);
+        }
         fence_mbar_init();
+        prefetch_tensormap(&tmap_q);
+        prefetch_tensormap(&tmap_k);
+        prefetch_tensormap(&tmap_v);
     }
     if (warp == 1) { tmem_alloc(smem_u32(&misc[0]), 512); tmem_relinquish(); }
-    if (!p.cu_seqlens) grid_wait();
-    const int32_t prefix = p.prefix ? min(n, p.prefix[g]) : 0;
-    const int32_t diagonal = min(q_block * kTiles + kTiles - 1, n_tiles - 1);
-    const int32_t n_kv = p.causal ? max(diagonal + 1, (prefix + kTile - 1) / kTile) : n_tiles;
-    // key tiles that the first query tile does not see: the block's first one, or none
-    const int skip = kTiles == 2 && p.causal && diagonal * kTile >= q0 + kTile && prefix <= diagonal * kTile ? 1 : 0;
-    auto tile_of = [&](int s) { return s <= diagonal ? diagonal - s : s; };
-    // the document's last V tile, if rows of another one follow in it
-    const int32_t ragged_tile = n % kTile != 0 && node0 + n < p.n_total ? n_tiles - 1 : -1;
-    const int kv_head = h / p.group;
-    auto load_k = [&](int s) {
-        const int st = s % kStages;
-        mbar_arrive_expect_tx(bar(kBarKFull + st), L::kTileBytes);
-        tma_load_3d(smem_u32(smem + L::kK + st * L::kTileBytes), &tmap_k, bar(kBarKFull + st), 0, kv_head, node0 + tile_of(s) * kTile);
-    };
-    auto load_v = [&](int s) {
-        const int st = s % kStages;
-        mbar_arrive_expect_tx(bar(kBarVFull + st), L::kTileBytes);
-        tma_load_3d(smem_u32(smem + L::kV + st * L::kTileBytes), &tmap_v, bar(kBarVFull + st), 0, kv_head, node0 + tile_of(s) * kTile);
-    };
-    if (tid == 0) {                          // the first tiles are on their way while the block is still setting up
-        mbar_arrive_expect_tx(bar(kBarQFull), kTiles * L::kTileBytes);
-        for (int t = 0; t < kTiles; ++t)
-            tma_load_3d(smem_u32(smem + L::kQ + t * L::kTileBytes), &tmap_q, bar(kBarQFull), 0, h, node0 + q0 + t * kTile);
-        load_k(0);
-        load_v(0);
-    }
-    if (p.early_release) grid_release();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = misc[0];
+    grid_wait();
+    if (p.early_release) grid_release();
+
+    // Item number k of this CTA, read by whole warps; false: there are no more.
+    auto take = [&](int k, Item& item) -> bool {
+        mbar_wait(bar(kBarItemFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 200);
+        item = items[k & 1];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(kBarItemEmpty + (k & 1)));
+        return item.n > 0 && *abort_flag == 0u;
+    };
 
     if (warp < 4) {
-        if constexpr (kTiles == 2) setmaxnreg_dec_32();
-        if (warp == 0) {
-            for (int s = 1; s < n_kv; ++s) {
-                mbar_wait(bar(kBarKEmpty + s % kStages), ((s / kStages) & 1) ^ 1, abort_flag, p.status, 210);
-                if (lane == 0) load_k(s);
-                mbar_wait(bar(kBarVEmpty + s % kStages), ((s / kStages) & 1) ^ 1, abort_flag, p.status, 211);
-                if (lane == 0) load_v(s);
+        if constexpr (kTiles == 2) setmaxnreg_dec_56();
+        if (warp == 2) {
+            // ---- the items: the CTA's own number, then what the counter gives, as late as its latency allows: the longest items come
+            // first, and who takes the short ones of the end is decided by who is done (two items ahead: causal 16 384 tokens 441 us, now @@) ----
+            int32_t index = (int32_t)blockIdx.x;
+            for (int k = 0;; ++k) {
+                if (k > 0) mbar_wait(bar(kBarFetch), (k - 1) & 1, abort_flag, p.status, 203);
+                Item item{};
+                while (item.n == 0) {
+                    if (index < 0) {
+                        uint32_t taken = (uint32_t)p.n_items;
+                        if (lane == 0 && (int32_t)gridDim.x < p.n_items) {
+                            taken = atomicAdd(p.next_item, 1u);
+                            // every item beyond the first ones is counted once, and every CTA's vain attempt: the last one leaves 0
+                            if (taken == (uint32_t)p.n_items - 1u) *p.next_item = 0u;
+                        }
+                        index = (int32_t)(gridDim.x + __shfl_sync(0xffffffffu, taken, 0));
+                    }
+                    if (index >= p.n_items) break;
+                    int32_t g, block;
+                    if (p.list) {
+                        const int4 entry = p.list[index / p.n_heads];
+                        g = entry.x;
+                        block = entry.y;
+                        item.node0 = entry.z;
+                        item.n = entry.x < 0 ? 0 : entry.w;
+                    } else {
+                        const int32_t row = index / p.n_heads;
+                        block = row / p.n_graphs;
+                        g = row % p.n_graphs;
+                        item.node0 = p.cu_seqlens ? p.cu_seqlens[g] : 0;
+                        item.n = p.cu_seqlens ? p.cu_seqlens[g + 1] - item.node0 : p.n_total;
+                    }
+                    item.head = index % p.n_heads;
+                    index = -1;
+                    const int32_t n_blocks = (item.n + kTiles * kTile - 1) / (kTiles * kTile);
+                    item.q_block = p.causal ? n_blocks - 1 - block : block;
+                    if (block >= n_blocks) item.n = 0;
+                    else item.prefix = p.prefix ? p.prefix[g] : 0;
+                }
+                if (k >= 2) mbar_wait(bar(kBarItemEmpty + (k & 1)), ((k >> 1) & 1) ^ 1, abort_flag, p.status, 201);
+                if (lane == 0) {
+                    items[k & 1] = item;
+                    mbar_arrive(bar(kBarItemFull + (k & 1)));
+                }
                 __syncwarp();
+                if (item.n == 0) break;
+            }
+        } else if (warp == 0) {
+            Item item;
+            Span span;
+            int c = 0;                                       // key tiles so far
+            for (int k = 0; take(k, item); ++k) {
+                span.set<kTiles>(item, p.causal);
+                const int kv_head = item.head / p.group;
+                if (k >= 2) mbar_wait(bar(kBarQEmpty + (k & 1)), ((k >> 1) & 1) ^ 1, abort_flag, p.status, 210);
+                if (lane == 0) {
+                    mbar_arrive_expect_tx(bar(kBarQFull + (k & 1)), span.tiles * L::kTileBytes);
+                    for (int t = 0; t < span.tiles; ++t)
+                        tma_load_3d(smem_u32(smem + L::kQ + (2 * (k & 1) + t) * L::kTileBytes), &tmap_q, bar(kBarQFull + (k & 1)), 0, item.head,
+                                    item.node0 + span.q0 + t * kTile);
+                }
+                const int32_t fetch = max(0, span.n_kv - 6);
+                for (int s = 0; s < span.n_kv; ++s, ++c) {
+                    if (s == fetch && lane == 0) mbar_arrive(bar(kBarFetch));
+                    const int st = c % kStages;
+                    const int32_t row = item.node0 + span.key_tile(s) * kTile;
+                    if (c >= kStages) mbar_wait(bar(kBarKEmpty + st), ((c / kStages) & 1) ^ 1, abort_flag, p.status, 211);
+                    if (lane == 0) {
+                        mbar_arrive_expect_tx(bar(kBarKFull + st), L::kTileBytes);
+                        tma_load_3d(smem_u32(smem + L::kK + st * L::kTileBytes), &tmap_k, bar(kBarKFull + st), 0, kv_head, row);
+                    }
+                    if (c >= kStages) mbar_wait(bar(kBarVEmpty + st), ((c / kStages) & 1) ^ 1, abort_flag, p.status, 212);
+                    if (lane == 0) {
+                        mbar_arrive_expect_tx(bar(kBarVFull + st), L::kTileBytes);
+                        tma_load_3d(smem_u32(smem + L::kV + st * L::kTileBytes), &tmap_v, bar(kBarVFull + st), 0, kv_head, row);
+                    }
+                    __syncwarp();
+                }
             }
         } else if (warp == 1) {
             constexpr uint32_t idesc_s = make_idesc_bf16(128, 128, false, false);
             const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
             const uint64_t desc_q0 = make_smem_desc(smem_u32(smem + L::kQ), L::kRowBytes, 0);
             const uint64_t desc_k0 = make_smem_desc(smem_u32(smem + L::kK), L::kRowBytes, 0);
-            mbar_wait(bar(kBarQFull), 0, abort_flag, p.status, 220);
-            for (int s = 0; s < n_kv; ++s) {
-                const int ks = s % kStages;
-                mbar_wait(bar(kBarKFull + ks), (s / kStages) & 1, abort_flag, p.status, 221);
+            Item item;
+            Span span;
+            int c = 0, step = 0;                             // key tiles, and score tiles, so far
+            int own[2][2] = {{-4, -4}, {-4, -4}}, done[2] = {0, 0};      // each query tile's last two steps, and how many there were
+            for (int k = 0; take(k, item); ++k) {
+                span.set<kTiles>(item, p.causal);
+                mbar_wait(bar(kBarQFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 220);
+                for (int s = 0; s < span.n_kv; ++s, ++c) {
+                    const int ks = c % kStages;
+                    mbar_wait(bar(kBarKFull + ks), (c / kStages) & 1, abort_flag, p.status, 221);
 #pragma unroll
-                for (int t = 0; t < kTiles; ++t) {
-                    if (kTiles == 2 && t == 0 && s < skip) continue;
-                    const int step = kTiles * s + t - skip, b = step % kBuffers;
-                    if (step >= kBuffers) mbar_wait(bar(kBarBufFree + b), (step / kBuffers - 1) & 1, abort_flag, p.status, 222);
-                    tc_fence_after();
-                    if (elect_one()) {
-                        const uint64_t da = advance_desc(desc_q0, t * L::kTileBytes), db = advance_desc(desc_k0, ks * L::kTileBytes);
+                    for (int t = 0; t < kTiles; ++t) {
+                        if (t >= span.tiles || (t == 0 && s < span.skip)) continue;
+                        const int b = step % kBuffers;
+                        if (step >= kBuffers) mbar_wait(bar(kBarBufFree + b), (step / kBuffers - 1) & 1, abort_flag, p.status, 222);
+                        // A tile's softmax may be one step behind, not two (see "one step apart" below): its last step but one has been through
+                        // its PV MMA.  Mostly that follows from the buffers; not where an item has one tile only.
+                        const int last_but_one = own[t][0], parity = done[t] & 1;
+                        if (step - last_but_one < kBuffers) mbar_wait(bar(kBarBufFree + last_but_one % kBuffers), (last_but_one / kBuffers) & 1, abort_flag, p.status, 223);
+                        own[t][0] = own[t][1];
+                        own[t][1] = step;
+                        ++done[t];
+                        ++step;
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const uint64_t da = advance_desc(desc_q0, (2 * (k & 1) + t) * L::kTileBytes), db = advance_desc(desc_k0, ks * L::kTileBytes);
 #pragma unroll
-                        for (int k = 0; k < D / 16; ++k)
-                            mma_ss(tm + b * 128, advance_desc(da, k * 32), advance_desc(db, k * 32), idesc_s, k > 0);
-                        mma_commit(bar(kBarSFull + b));
-                        if (t == kTiles - 1) mma_commit(bar(kBarKEmpty + ks));
+                            for (int e = 0; e < D / 16; ++e)
+                                mma_ss(tm + b * 128, advance_desc(da, e * 32), advance_desc(db, e * 32), idesc_s, e > 0);
+                            mma_commit(bar(kBarSFull + 2 * t + parity));
+                            if (t == span.tiles - 1) {
+                                mma_commit(bar(kBarKEmpty + ks));
+                                if (s == span.n_kv - 1) mma_commit(bar(kBarQEmpty + (k & 1)));
+                            }
+                        }
+                        __syncwarp();
                     }
-                    __syncwarp();
                 }
             }
-        } else if (warp == 3) {
+        } else {
             constexpr uint32_t idesc_o = make_idesc_bf16(128, D, false, true);
             const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
             const uint64_t desc_v0 = make_smem_desc(smem_u32(smem + L::kV), L::kRowBytes, 0);
-            for (int s = 0; s < n_kv; ++s) {
-                const int vs = s % kStages;
-                mbar_wait(bar(kBarVFull + vs), (s / kStages) & 1, abort_flag, p.status, 230);
-                if (tile_of(s) == ragged_tile) {
-                    clear_rows(smem + L::kV + vs * L::kTileBytes, n - ragged_tile * kTile, L::kRowBytes);
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                }
-                const uint64_t dv = advance_desc(desc_v0, vs * L::kTileBytes);
-#pragma unroll
-                for (int t = 0; t < kTiles; ++t) {
-                    if (kTiles == 2 && t == 0 && s < skip) continue;
-                    const int b = (kTiles * s + t - skip) % kBuffers, own = t == 0 ? s - skip : s;       // own: the query tile's steps so far
-                    mbar_wait(bar(kBarPFull + 2 * t + (own & 1)), (own >> 1) & 1, abort_flag, p.status, 232);
-                    tc_fence_after();
-                    if (elect_one()) {
-#pragma unroll
-                        for (int k = 0; k < kTile / 16; ++k)      // P of key half hf sits at the start of that half's score columns
-                            mma_ts(tm + kOCol + t * 64, tm + b * 128 + (k / 4) * kCols + (k % 4) * 8, advance_desc(dv, k * 16 * L::kRowBytes), idesc_o,
-                                   own > 0 || k > 0 ? 1u : 0u);
-                        mma_commit(bar(kBarODone + 2 * t + (own & 1)));
-                        mma_commit(bar(kBarBufFree + b));
-                        if (t == kTiles - 1) mma_commit(bar(kBarVEmpty + vs));
+            Item item;
+            Span span;
+            int c = 0, step = 0, own[2] = {0, 0};            // key tiles, score tiles and each query tile's so far
+            for (int k = 0; take(k, item); ++k) {
+                span.set<kTiles>(item, p.causal);
+                // the document's last V tile, if rows of another one follow in it
+                const int32_t ragged_tile = item.n % kTile != 0 && item.node0 + item.n < p.n_total ? item.n / kTile : -1;
+                for (int s = 0; s < span.n_kv; ++s, ++c) {
+                    const int vs = c % kStages;
+                    mbar_wait(bar(kBarVFull + vs), (c / kStages) & 1, abort_flag, p.status, 230);
+                    if (span.key_tile(s) == ragged_tile) {
+                        clear_rows(smem + L::kV + vs * L::kTileBytes, item.n - ragged_tile * kTile, L::kRowBytes);
+                        fence_proxy_async_smem();
+                        __syncwarp();
                     }
-                    __syncwarp();
+                    const uint64_t dv = advance_desc(desc_v0, vs * L::kTileBytes);
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t) {
+                        if (t >= span.tiles || (t == 0 && s < span.skip)) continue;
+                        const int b = step % kBuffers;
+                        const uint32_t begun = s > (t == 0 ? span.skip : 0) ? 1u : 0u;
+                        mbar_wait(bar(kBarPFull + 2 * t + (own[t] & 1)), (own[t] >> 1) & 1, abort_flag, p.status, 231);
+                        tc_fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int e = 0; e < kTile / 16; ++e)      // P of key half hf sits at the start of that half's score columns
+                                mma_ts(tm + kOCol + t * 64, tm + b * 128 + (e / 4) * kCols + (e % 4) * 8, advance_desc(dv, e * 16 * L::kRowBytes), idesc_o,
+                                       e > 0 ? 1u : begun);
+                            mma_commit(bar(kBarODone + 2 * t + (own[t] & 1)));
+                            mma_commit(bar(kBarBufFree + b));
+                            if (t == span.tiles - 1) mma_commit(bar(kBarVEmpty + vs));
+                        }
+                        __syncwarp();
+                        ++step;
+                        ++own[t];
+                    }
                 }
             }
         }
     } else {
         // =================================== softmax warps ===================================
-        if constexpr (kTiles == 2) setmaxnreg_inc_112();
+        if constexpr (kTiles == 2) setmaxnreg_inc_104();
         const int sw = warp - 4;
         const int t = sw >> 3, hf = (sw >> 2) & 1;
         const int r = ((warp & 3) << 5) | lane;
@@ -249,39 +369,52 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         const uint32_t tO = tmem + kOCol + t * 64 + hf * kOC + lane_off;
         const uint32_t pair_bar = kNbPair + t * 4 + (warp & 3);
         float* xchg = (float*)(smem + L::kXchg) + t * 512;
-        const int32_t q = q0 + t * kTile + r;                                   // this thread's query
-        const int32_t limit = row_limit(p.causal, q, prefix, n);
-        const int32_t least_limit = row_limit(p.causal, q0 + t * kTile + (warp & 3) * 32, prefix, n);        // of the warp's rows
-        const int32_t first = t == 0 ? skip : 0;
+        const uint64_t c1c1 = both(p.c1);
+        [[maybe_unused]] const uint64_t to_tanh2 = both(p.to_tanh);
+
+        int step0 = 0, own = 0;                 // score tiles, and this query tile's, so far
+        for (int k = 0;; ++k) {
+        // (the item is read again where its results are written, and given back behind that: fewer registers in between)
+        mbar_wait(bar(kBarItemFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 202);
+        if (items[k & 1].n == 0 || *abort_flag != 0u) break;
+        Span span;
+        span.set<kTiles>(items[k & 1], p.causal);
+        const int32_t first = t == 0 ? span.skip : 0, diagonal = span.diagonal, step_by = span.tiles;
+        int32_t key_tile = span.key_tile(first), left = t < span.tiles ? span.n_kv - first : 0;       // left: steps
+        int step = step0 + (span.tiles == 2 ? 2 * first + t - span.skip : 0);
+        step0 += span.steps();
+        if (left > 0) {
+        const int32_t q = span.q0 + t * kTile + r;                                     // this thread's query
+        const int32_t limit = row_limit(p.causal, q, items[k & 1].prefix, items[k & 1].n);
+        const bool counts = q < items[k & 1].n;
+        bool begins = true;
         float m = 0.f, l = 0.f;
         [[maybe_unused]] float l_rounded = 0.f;
         bool wide = false;                               // kCap: a score was out of the polynomial's reach
-        const uint64_t c1c1 = both(p.c1);
-        [[maybe_unused]] const uint64_t to_tanh2 = both(p.to_tanh);
-        [[maybe_unused]] const float slope2 = kSlope ? p.slopes[h] * kLog2e : 0.f;
+        [[maybe_unused]] const float slope2 = kSlope ? p.slopes[items[k & 1].head] * kLog2e : 0.f;
+        [[maybe_unused]] const int32_t prefix = kSlope ? items[k & 1].prefix : 0;
 
         uint32_t sa[kCW], sb[kCW];              // score chunks, alternating
         uint32_t tS = 0;                        // this thread's score columns of the current step
         auto load_chunk = [&](int c, uint32_t (&sr)[kCW]) { tmem_ld16(tS + c * kCW, sr); };
         // first chunk of a step's scores: fetched at the end of the step before, behind the P store
-        auto begin_step = [&](int s) {
-            const int step = kTiles * s + t - skip, b = step % kBuffers;
+        auto begin_step = [&]() {
+            const int b = step % kBuffers;
             tS = tmem + b * 128 + hf * kCols + lane_off;
-            mbar_wait(bar(kBarSFull + b), (step / kBuffers) & 1, abort_flag, p.status, 250);
+            mbar_wait(bar(kBarSFull + 2 * t + (own & 1)), (own >> 1) & 1, abort_flag, p.status, 250);
             tc_fence_after();
             load_chunk(0, sa);
         };
-        begin_step(first);
+        begin_step();
 
-        for (int s = first; s < n_kv; ++s) {
-            const int own = s - first;
-            const int32_t kv0 = tile_of(s) * kTile + hf * kCols;       // this thread's first key
-            const bool ragged = kv0 + kCols > least_limit;             // some row of the warp does not see all of the columns
+        for (;;) {
+            const int32_t kv0 = key_tile * kTile + hf * kCols;         // this thread's first key
             const int valid = limit - kv0;                             // columns that this thread's row sees (may be <= 0)
+            const bool ragged = __any_sync(0xffffffffu, valid < kCols);
+            [[maybe_unused]] const int32_t row0 = q - lane;
             // Penalty on distance.  Where no key lies behind the query (or, for masked ones, it does not matter) it is linear in the
             // column: (key - query) slope.  Otherwise keys behind all of the warp's rows have it the other way round, and in between
             // a distance is made for every element.
-            const int32_t row0 = q0 + t * kTile + (warp & 3) * 32;
             const bool before = kv0 + kCols - 1 <= row0 || (p.causal && kv0 >= prefix), behind = kv0 >= row0 + 31;
             [[maybe_unused]] const bool mixed = kSlope && !before && !behind;
             [[maybe_unused]] const float step_slope = before ? slope2 : -slope2;
@@ -292,7 +425,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             bool exact = false;                    // take the tile maximum first
 
             // Is the starting reference in reach of the first tile?  Four of the thread's first 16 scores tell.
-            if (own == 0) {
+            if (begins) {
                 tmem_wait_ld();
                 float top = -INFINITY;
 #pragma unroll
@@ -302,7 +435,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     if constexpr (kSlope) x -= slope2 * fabsf((float)(kv0 + 4 * i - q));
                     if (4 * i < valid) top = fmaxf(top, x);
                 }
-                exact = named_barrier_or(pair_bar, 64, valid > 0 && q < n && !(fabsf(top) <= kPeekReach));   // (a half without valid columns has no say)
+                exact = named_barrier_or(pair_bar, 64, valid > 0 && counts && !(fabsf(top) <= kPeekReach));   // (a half without valid columns has no say)
             }
 
             // Scores of eight consecutive columns in log2 units, plus `add`; general: any score, any distance.
@@ -367,11 +500,11 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     xchg[hf * 128 + r] = mx;
                     named_barrier_sync(pair_bar, 64);
                     mx = fmaxf(mx, xchg[(hf ^ 1) * 128 + r]);
-                    const float m_new = own == 0 ? ceilf(mx) : fmaxf(m, ceilf(mx));
-                    const float alpha = own == 0 ? 0.f : ex2_approx(m - m_new);      // (there is nothing yet; a first reference far below 0 would give infinity)
+                    const float m_new = begins ? ceilf(mx) : fmaxf(m, ceilf(mx));
+                    const float alpha = begins ? 0.f : ex2_approx(m - m_new);      // (there is nothing yet; a first reference far below 0 would give infinity)
                     l *= alpha;
                     if constexpr (kExact) l_rounded *= alpha;
-                    if (own > 0) {
+                    if (!begins) {
                         mbar_wait(bar(kBarODone + 2 * t + ((own - 1) & 1)), ((own - 1) >> 1) & 1, abort_flag, p.status, 251);
                         tc_fence_after();
                         uint32_t o[kOC];
@@ -424,8 +557,8 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 if (exact) break;
                 // reference too low for some row of this pair of warps?  Also catches inf / NaN, and scores near the cap.
                 // (Rows behind the document have no say.)
-                const bool beyond = kCap && !wide && q < n && !(top_u <= kTanhReach);
-                if (!named_barrier_or(pair_bar, 64, (q < n && !(tile_sum <= kSumThreshold)) || beyond)) break;
+                const bool beyond = kCap && !wide && counts && !(top_u <= kTanhReach);
+                if (!named_barrier_or(pair_bar, 64, (counts && !(tile_sum <= kSumThreshold)) || beyond)) break;
                 if (kCap && !wide && named_barrier_or(pair_bar, 64, beyond)) wide = true;       // from now on, with the tanh of any score
                 else exact = true;
             }
@@ -441,16 +574,20 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             tmem_wait_st();
             tc_fence_before();
             // Warps of a tile can be one step apart (nothing in the speculative pass waits for the previous PV MMA), so odd and even steps
-            // have barriers of their own: a parity wait can only tell two states apart.  Two steps apart is impossible, because the S MMA
-            // needs a score buffer that is only freed after the PV MMA.
+            // have barriers of their own: a parity wait can only tell two states apart.  Two steps apart they are never: the S MMA waits
+            // for the PV MMA of the last step but one.
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(kBarPFull + 2 * t + (own & 1)));
-            if (s + 1 < n_kv) begin_step(s + 1);
+            ++own;
+            step += step_by;
+            begins = false;
+            if (--left == 0) break;
+            key_tile = key_tile > diagonal ? key_tile + 1 : key_tile > 0 ? key_tile - 1 : diagonal + 1;
+            begin_step();
         }
 
         // ---- epilogue: O / l, LSE ----
-        const int last = n_kv - 1 - first;
-        mbar_wait(bar(kBarODone + 2 * t + (last & 1)), (last >> 1) & 1, abort_flag, p.status, 252);
+        mbar_wait(bar(kBarODone + 2 * t + ((own - 1) & 1)), ((own - 1) >> 1) & 1, abort_flag, p.status, 252);
         tc_fence_after();
         xchg[256 + hf * 128 + r] = l;
         if constexpr (kExact) xchg[hf * 128 + r] = l_rounded;
@@ -460,12 +597,13 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         uint32_t o[kOC];
         if constexpr (kOC == 32) tmem_ld32(tO, o); else tmem_ld16(tO, o);
         tmem_wait_ld();
-        if (q < n) {
+        if (counts) {
+            const int32_t node = items[k & 1].node0 + q, h = items[k & 1].head;
             float x[kOC];
             if constexpr (kExact) {
 #pragma unroll
                 for (int i = 0; i < kOC; ++i) x[i] = __uint_as_float(o[i]) / l_rounded;      // (a row with one key gets that key's value to the bit)
-                float4* dst32 = (float4*)(p.out_f32 + ((size_t)(node0 + q) * p.n_heads + h) * D + hf * kOC);
+                float4* dst32 = (float4*)(p.out_f32 + ((size_t)node * p.n_heads + h) * D + hf * kOC);
 #pragma unroll
                 for (int i = 0; i < kOC / 4; ++i) dst32[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
             } else {
@@ -473,12 +611,16 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 #pragma unroll
                 for (int i = 0; i < kOC; ++i) x[i] = __uint_as_float(o[i]) * inv_l;
             }
-            uint4* dst = (uint4*)(p.out + ((size_t)(node0 + q) * p.n_heads + h) * D + hf * kOC);
+            uint4* dst = (uint4*)(p.out + ((size_t)node * p.n_heads + h) * D + hf * kOC);
 #pragma unroll
             for (int i = 0; i < kOC / 8; ++i)
                 dst[i] = make_uint4(pack_bf16x2(x[8 * i], x[8 * i + 1]), pack_bf16x2(x[8 * i + 2], x[8 * i + 3]), pack_bf16x2(x[8 * i + 4], x[8 * i + 5]),
                                     pack_bf16x2(x[8 * i + 6], x[8 * i + 7]));
-            if (hf == 0) p.lse[(size_t)h * p.n_total + node0 + q] = (m + log2f(l)) * kLn2;
+            if (hf == 0) p.lse[(size_t)h * p.n_total + node] = (m + log2f(l)) * kLn2;
+        }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(kBarItemEmpty + (k & 1)));
         }
     }
 
@@ -491,14 +633,14 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 
 // Work list of a packed batch, a warp per document.
 constexpr int kListThreads = 128;
-__global__ void __launch_bounds__(kListThreads) position_list_kernel(int4* list, int32_t entries, const int32_t* cu_seqlens, int32_t n_graphs)
+__global__ void __launch_bounds__(kListThreads) position_list_kernel(int4* list, int32_t entries, const int32_t* cu_seqlens, int32_t n_graphs, int32_t causal)
 {
     grid_wait();
     grid_release();
     const int32_t w = (int32_t)((blockIdx.x * blockDim.x + threadIdx.x) >> 5);
-    if (w < n_graphs) write_work_list<2 * kTile>(list, entries, cu_seqlens, n_graphs, w);
+    if (w < n_graphs) write_list<2 * kTile>(list, entries, cu_seqlens, n_graphs, w, causal);
 }
-constexpr size_t kListMinSaved = 2048;       // blocks of the plain grid that the list has to save: it costs a launch
+constexpr size_t kListMinSaved = 256;        // empty items that the list has to save: it costs a launch
 
 template <int D, bool kCap, bool kSlope, bool kExact>
 gt_status launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, PositionFwdParams p, const gt_batch* batch, int32_t rows,
@@ -509,9 +651,8 @@ gt_status launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap
     static std::atomic<uint64_t> granted[2] = {};
     const gt_status st = grant_smem(kern, granted[one], Smem<D>::kDynamic);
     if (st != GT_OK) return st;
-    const dim3 grid = p.list ? dim3((unsigned)(list_entries(batch, rows) * p.n_heads))
-                             : dim3((unsigned)p.n_heads, (unsigned)((batch->max_seqlen + rows - 1) / rows), (unsigned)batch->n_graphs);
-    p.early_release = (int64_t)grid.x * grid.y * grid.z <= sm_count();
+    const dim3 grid((unsigned)std::min(p.n_items, sm_count()));
+    p.early_release = p.n_items <= sm_count();
     return launch_overlapped(kern, grid, 128 + 2 * rows, Smem<D>::kDynamic, s, tq, tk, tv, p);
 }
 
@@ -553,6 +694,7 @@ extern "C" gt_status gt_position_attn_fwd(const void* q, const void* k, const vo
     p.out_f32 = out_f32;
     p.lse = lse;
     p.status = (uint32_t*)workspace;
+    p.next_item = (uint32_t*)workspace + kNextForward;
     p.n_total = batch->n_total;
     p.n_heads = n_heads;
     p.group = n_heads / n_kv_heads;
@@ -563,14 +705,19 @@ extern "C" gt_status gt_position_attn_fwd(const void* q, const void* k, const vo
     cudaStream_t s = (cudaStream_t)stream;
     // Blocks of one query tile where those of two would leave half of the SMs idle or more.
     const int32_t rows = (int64_t)((batch->max_seqlen + kTile - 1) / kTile) * batch->n_graphs * n_heads <= sm_count() ? kTile : 2 * kTile;
+    p.n_graphs = batch->n_graphs;
+    int64_t n_items = (int64_t)((batch->max_seqlen + rows - 1) / rows) * batch->n_graphs * n_heads;
     if (batch->n_graphs > 1 && rows == 2 * kTile && list_saves(batch, rows, n_heads, kListMinSaved)) {
         int4* list = (int4*)((uint8_t*)workspace + kHeaderBytes);
         p.list = list;
+        n_items = (int64_t)list_entries(batch, rows) * n_heads;
         const unsigned blocks = (unsigned)((batch->n_graphs + kListThreads / 32 - 1) / (kListThreads / 32));
         if ((st = launch_overlapped(position_list_kernel, dim3(blocks), kListThreads, 0, s, list, (int32_t)list_entries(batch, rows), batch->cu_seqlens,
-                                    batch->n_graphs)) != GT_OK)
+                                    batch->n_graphs, p.causal)) != GT_OK)
             return st;
     }
+    if (n_items > 0x7fff0000) return GT_ERR_UNSUPPORTED;
+    p.n_items = (int32_t)n_items;
     auto go = [&](auto wide, auto capped, auto sloped) {
         constexpr int D = decltype(wide)::value ? 64 : 32;
         constexpr bool kCap = decltype(capped)::value, kSlope = decltype(sloped)::value;
