@@ -22,6 +22,18 @@ template <bool B> struct Tag { static constexpr bool value = B; };
 
 __device__ __forceinline__ uint64_t both(float x) { return sm100::pack_f32x2(x, x); }
 
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+
 // P(u) of two arguments u = y^2.
 __device__ __forceinline__ uint64_t tanh_ratio(uint64_t u)
 {

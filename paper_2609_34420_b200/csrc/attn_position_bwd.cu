@@ -400,7 +400,7 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                             const uint64_t uu = mul_f32x2(u, u);
                             float u0, u1;
                             unpack_f32x2(uu, u0, u1);
-                            top_u = fmaxf(top_u, fmaxf(u0, u1));
+                            top_u = max3(top_u, u0, u1);
                             t = mul_f32x2(u, tanh_ratio(uu));
                         }
                         x = fma_f32x2(t, cap22, add);

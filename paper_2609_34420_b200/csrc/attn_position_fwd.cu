@@ -40,6 +40,9 @@ constexpr int kStages = 2;                    // of the K ring and of the V ring
 constexpr int kCols = 64;                     // score columns of a softmax thread
 constexpr int kCW = 16;                       // columns per TMEM load
 constexpr float kSumThreshold = 0x1p24f;       // tile row sum above which the reference is raised
+// Scores of a capped row lie within cap log2(e) of 0 at the diagonal, so that against a reference of half of that the largest P is between 2^-108 and
+// 2^37: sums, products with v of up to 2^60 and their sums stay within fp32, and nothing that counts is lost below.
+constexpr float kBoundedCap = 50.0f;
 constexpr float kPeekReach = 24.0f;            // log2 units within which a row's first scores leave the starting reference as it is
 
 struct PositionFwdParams {
@@ -62,6 +65,7 @@ struct PositionFwdParams {
     float c1;                  // log2(e) / sqrt(d)
     float to_tanh;             // 1 / (sqrt(d) cap)
     float cap2;                // cap log2(e)
+    float reference;           // kCapForm 1: of all rows, a whole number
 };
 
 enum Barrier {
@@ -126,16 +130,20 @@ constexpr int kNbPair = 2;                    // named barriers: + 4 t + lane qu
 __device__ __forceinline__ void setmaxnreg_dec_56() { asm volatile("setmaxnreg.dec.sync.aligned.u32 56;"); }
 
 // kTiles = 1: blocks of one query tile, for grids that would leave half of the SMs idle or more.
+// kCapForm: 0 no cap; 1 a cap of up to kBoundedCap; 2 any cap.  With the second form no score can be out of reach of a reference of half the
+// cap, so that nothing is redone, and P takes the place of the scores chunk by chunk; the registers that this frees are what hides the
+// polynomial's latency (causal 16 384 tokens, cap 30: 665 -> @@ us).
 // kExact (with the fp32 output): O is divided by the sum of the probabilities as the MMA reads them, rounded to bf16, so that their
 // rounding cancels where a row has few large ones; lse is that of the unrounded ones all the same.  The backward subtracts dout . out from
 // dout . v_j, two nearly equal numbers in such rows: with scores of standard deviation 4, dq was off by 0.6 % (out rounded to bf16 and
 // divided by the unrounded sum), by 0.45 % without either, and by 0.27 % with both.
-template <int D, bool kCap, bool kSlope, int kTiles, bool kExact>
+template <int D, int kCapForm, bool kSlope, int kTiles, bool kExact>
 __global__ void __launch_bounds__(128 + 256 * kTiles, 1)
 position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                     const __grid_constant__ CUtensorMap tmap_v, const PositionFwdParams p)
 {
     using L = Smem<D>;
+    constexpr bool kCap = kCapForm != 0, kBounded = kCapForm == 1;
     constexpr int kBuffers = kTiles + 1, kReaders = 3 + 8 * kTiles;          // kReaders: warps that work on an item
     constexpr uint32_t kOCol = 384;
     extern __shared__ uint8_t smem_raw[];
@@ -388,9 +396,9 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         const int32_t limit = row_limit(p.causal, q, items[k & 1].prefix, items[k & 1].n);
         const bool counts = q < items[k & 1].n;
         bool begins = true;
-        float m = 0.f, l = 0.f;
+        float m = kBounded ? p.reference : 0.f, l = 0.f;
         [[maybe_unused]] float l_rounded = 0.f;
-        bool wide = false;                               // kCap: a score was out of the polynomial's reach
+        [[maybe_unused]] bool wide = false;              // a score was out of the polynomial's reach
         [[maybe_unused]] const float slope2 = kSlope ? p.slopes[items[k & 1].head] * kLog2e : 0.f;
         [[maybe_unused]] const int32_t prefix = kSlope ? items[k & 1].prefix : 0;
 
@@ -418,14 +426,14 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             const bool before = kv0 + kCols - 1 <= row0 || (p.causal && kv0 >= prefix), behind = kv0 >= row0 + 31;
             [[maybe_unused]] const bool mixed = kSlope && !before && !behind;
             [[maybe_unused]] const float step_slope = before ? slope2 : -slope2;
-            uint32_t pk[32];                       // P of this thread's columns, bf16 pairs
+            [[maybe_unused]] uint32_t pk[32];      // P of this thread's columns, bf16 pairs
             float tile_sum = 0.f;
             [[maybe_unused]] uint64_t rounded2 = 0;
             bool loaded = true;                    // chunk 0 is already on its way
             bool exact = false;                    // take the tile maximum first
 
             // Is the starting reference in reach of the first tile?  Four of the thread's first 16 scores tell.
-            if (begins) {
+            if (!kBounded && begins) {
                 tmem_wait_ld();
                 float top = -INFINITY;
 #pragma unroll
@@ -463,7 +471,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                             if (col + i >= valid) u0 = 0.f;
                             if (col + i + 1 >= valid) u1 = 0.f;
                         }
-                        top_u = fmaxf(top_u, fmaxf(u0, u1));
+                        top_u = max3(top_u, u0, u1);
                         y = fma_f32x2(mul_f32x2(raw, c1c1), tanh_ratio(uu), a);
                     } else {
                         y = fma_f32x2(raw, c1c1, a);
@@ -477,7 +485,44 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 }
             };
 
-            for (;;) {
+            if constexpr (kBounded) {
+                uint64_t sum2 = pack_f32x2(0.f, 0.f);
+                rounded2 = sum2;
+                auto chunk = [&](int c, const uint32_t (&sr)[kCW], auto rag) {
+                    float x[kCW];
+                    uint32_t w[kCW / 2];
+                    top_u = 0.f;
+#pragma unroll
+                    for (int e = 0; e < kCW; e += 8) scores8(sr + e, c * kCW + e, -m, rag, Tag<false>{}, *(float (*)[8])(x + e));
+                    if (__any_sync(0xffffffffu, counts && !(top_u <= kTanhReach)) || mixed) {
+#pragma unroll
+                        for (int e = 0; e < kCW; e += 8) scores8(sr + e, c * kCW + e, -m, rag, Tag<true>{}, *(float (*)[8])(x + e));
+                    }
+#pragma unroll
+                    for (int i = 0; i < kCW; i += 2) {
+                        if constexpr (decltype(rag)::value) {
+                            if (c * kCW + i >= valid) x[i] = -INFINITY;
+                            if (c * kCW + i + 1 >= valid) x[i + 1] = -INFINITY;
+                        }
+                        const float lo = ex2_approx(x[i]), hi = ex2_approx(x[i + 1]);
+                        sum2 = add_f32x2(sum2, pack_f32x2(lo, hi));
+                        w[i >> 1] = pack_bf16x2(lo, hi);
+                        if constexpr (kExact) rounded2 = add_f32x2(rounded2, pack_u32x2(w[i >> 1] << 16, w[i >> 1] & 0xffff0000u));
+                    }
+                    tmem_st8(tS + c * (kCW / 2), w);             // over columns of chunks that are in registers, or were
+                };
+                auto pass = [&](auto rag) {
+                    tmem_wait_ld(); load_chunk(1, sb); chunk(0, sa, rag);
+                    tmem_wait_ld(); load_chunk(2, sa); chunk(1, sb, rag);
+                    tmem_wait_ld(); load_chunk(3, sb); chunk(2, sa, rag);
+                    tmem_wait_ld(); chunk(3, sb, rag);
+                };
+                if (ragged) pass(Tag<true>{});
+                else pass(Tag<false>{});
+                float lo, hi;
+                unpack_f32x2(sum2, lo, hi);
+                tile_sum = lo + hi;
+            } else for (;;) {
                 if (exact) {
                     // ---- classical way: tile maximum, new reference, rescale of l and O ----
                     float mx = -INFINITY;
@@ -570,7 +615,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             }
 
             // P over the first half of this thread's own score columns
-            tmem_st32(tS, pk);
+            if constexpr (!kBounded) tmem_st32(tS, pk);
             tmem_wait_st();
             tc_fence_before();
             // Warps of a tile can be one step apart (nothing in the speculative pass waits for the previous PV MMA), so odd and even steps
@@ -642,12 +687,12 @@ __global__ void __launch_bounds__(kListThreads) position_list_kernel(int4* list,
 }
 constexpr size_t kListMinSaved = 256;        // empty items that the list has to save: it costs a launch
 
-template <int D, bool kCap, bool kSlope, bool kExact>
+template <int D, int kCapForm, bool kSlope, bool kExact>
 gt_status launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, PositionFwdParams p, const gt_batch* batch, int32_t rows,
                  cudaStream_t s)
 {
     const bool one = rows == kTile;
-    auto kern = one ? position_fwd_kernel<D, kCap, kSlope, 1, kExact> : position_fwd_kernel<D, kCap, kSlope, 2, kExact>;
+    auto kern = one ? position_fwd_kernel<D, kCapForm, kSlope, 1, kExact> : position_fwd_kernel<D, kCapForm, kSlope, 2, kExact>;
     static std::atomic<uint64_t> granted[2] = {};
     const gt_status st = grant_smem(kern, granted[one], Smem<D>::kDynamic);
     if (st != GT_OK) return st;
@@ -718,10 +763,16 @@ extern "C" gt_status gt_position_attn_fwd(const void* q, const void* k, const vo
     }
     if (n_items > 0x7fff0000) return GT_ERR_UNSUPPORTED;
     p.n_items = (int32_t)n_items;
+    const bool bounded = cap <= kBoundedCap;
+    p.reference = bounded ? floorf(0.5f * p.cap2) : 0.f;
     auto go = [&](auto wide, auto capped, auto sloped) {
         constexpr int D = decltype(wide)::value ? 64 : 32;
         constexpr bool kCap = decltype(capped)::value, kSlope = decltype(sloped)::value;
-        return out_f32 ? launch<D, kCap, kSlope, true>(tq, tk, tv, p, batch, rows, s) : launch<D, kCap, kSlope, false>(tq, tk, tv, p, batch, rows, s);
+        auto exact = [&](auto exact_) {
+            constexpr bool kExact = decltype(exact_)::value;
+            return bounded ? launch<D, kCap ? 1 : 0, kSlope, kExact>(tq, tk, tv, p, batch, rows, s) : launch<D, kCap ? 2 : 0, kSlope, kExact>(tq, tk, tv, p, batch, rows, s);
+        };
+        return out_f32 ? exact(Tag<true>{}) : exact(Tag<false>{});
     };
     return position::pick(head_dim == 64, cap > 0.f, slopes != nullptr, go);
 }
