@@ -1,6 +1,8 @@
 // gt_position_attn_bwd: gradient of attention over packed token sequences with respect to q, k and v (formulas: the header).
 //
-// One CTA owns one query head and one tile of 128 keys and walks over the query tiles that see any of them.  Scores are recomputed
+// An item of work is one query head and one tile of 128 keys, for which a CTA walks over the query tiles that see any of them.  The grid
+// is persistent: a CTA takes one item after the other, and its warps run through them as through one long row of query tiles, so that the
+// next item's rows arrive, and its first scores are made, while the last one's dK and dV are written.  Scores are recomputed
 // TRANSPOSED (S^T = K Q^T, thread = key = TMEM lane), so that P^T and dS^T can go straight back to tensor memory as the A operands of
 // dV += P^T dO and dK += dS^T Q; dS^T is also written to shared memory (MN-major A operand) for dQ_i = dS K, which is added to an fp32
 // accumulator in global memory.  A mask is a range of queries for every key, so a thread compares column numbers with two bounds.
@@ -13,8 +15,8 @@
 // half's warps compute.  Three helper warps issue the MMAs; each accumulator and each part of a TMEM stage belongs to one of them, so
 // every reuse of tensor memory follows, in that thread's issue order, the MMA that reads the old contents.
 //
-//   warp 0        TMA producer: K, V once; Q_i, dO_i and the per-query rows through a 2-stage ring; clears what lies behind the document
-//   warps 1, 3, 2 MMA issuers: dV and the next S^T; dK and the next dP^T; dQ
+//   warp 0        fetches the items; TMA producer: K and V of an item; Q_i, dO_i and the per-query rows through a 2-stage ring
+//   warps 1, 3, 2 MMA issuers: dV and the next S^T; dK and the next dP^T; dQ (which also clears what lies behind the document)
 //   warps 4-19    softmax: warps 4-11 own queries [0,64) of every tile, warps 12-19 queries [64,128); within a half, four warps per 32
 //                 query columns
 //   warps 20-23   dQ reducer: TMEM -> shared memory -> TMA reduce-add into the fp32 accumulator
@@ -22,6 +24,8 @@
 // TMEM columns, half g: S^T/P^T [128g, 128g+64)  dP^T/dS^T [128g+64, 128g+128);
 //               dV [256,320)  dK [320,384)  dQ [384,448)  K [448,480)  V [480,512) (bf16 pairs).
 #include <math.h>
+
+#include <algorithm>
 
 #include "attn_position.cuh"
 
@@ -50,7 +54,10 @@ struct PositionBwdParams {
     float* dk_acc;           // [T,G,D] fp32 (workspace, zeroed) where heads share keys, else nullptr
     float* dv_acc;
     uint32_t* status;
-    const int4* list;        // packed batch: work list; block index = entry * heads + head (nullptr: grid of heads x tiles x documents)
+    uint32_t* next_item;     // counts the items that have been taken beyond the grid's first ones; 0 before and after the kernel
+    const int4* list;        // packed batch: work list; item = entry * heads + head (nullptr: heads, then documents, then tiles)
+    int32_t n_items;
+    int32_t n_graphs;
     int32_t n_total;
     int32_t n_heads;
     int32_t group;           // query heads per key head
@@ -63,8 +70,13 @@ struct PositionBwdParams {
 };
 
 enum Barrier {
-    kBarKvFull = 0,
-    kBarQdoFull = 1,                         // [2]  Q_i, dO_i and the per-query rows of tile i
+    kBarItemFull = 0,                        // [2]  an item's description
+    kBarItemEmpty = kBarItemFull + 2,        // [2]  all warps that work on it are done with it
+    kBarKFull = kBarItemEmpty + 2,           // [2]  K of an item
+    kBarKEmpty = kBarKFull + 2,              // [2]  commit behind the item's last dQ MMA
+    kBarVFull = kBarKEmpty + 2,              //      V of an item
+    kBarVEmpty,                              //      4 warp arrivals: V rows copied to tensor memory
+    kBarQdoFull,                             // [2]  Q_i, dO_i and the per-query rows of tile i
     kBarStageEmpty = kBarQdoFull + kStages,  // [2]  commits behind the last MMAs that read Q_i / dO_i
     kBarSFull = kBarStageEmpty + kStages,    // [2]  per half: S^T of the next tile is in tensor memory
     kBarDpFull = kBarSFull + 2,              // [2]  per half: dP^T of the next tile
@@ -73,9 +85,9 @@ enum Barrier {
     kBarDqFull = kBarDsReady + 2,
     kBarDqFree,
     kBarKvTmem,                              //      8 warp arrivals: K and V rows copied to tensor memory
-    kBarKClear,                              //      K's rows behind the document are cleared
-    kBarQClear,                              //      ... and those of the last Q and dO tiles
-    kBarFinal,
+    kBarQClear,                              //      the rows of a Q and a dO tile behind the document are cleared
+    kBarFinal,                               //      dV and dK of an item
+    kBarAccFree,                             //      16 warp arrivals: they have been read
     kNumBarriers
 };
 constexpr int kNbDqStaged = 4, kNbDqStagingFree = 5;       // named barriers
@@ -84,24 +96,34 @@ template <int D>
 struct Smem {
     static constexpr int kRowBytes = D * 2;
     static constexpr int kTileBytes = 128 * kRowBytes;
-    static constexpr int kK = 0;
-    static constexpr int kV = kK + kTileBytes;
+    static constexpr int kK = 0;                                    // [2 items]
+    static constexpr int kV = kK + 2 * kTileBytes;
     static constexpr int kOnes = kV + kTileBytes;                   // two constant groups of 8 x 16 bf16 (256 B each)
     static constexpr int kStageBytes = 2 * kTileBytes;              // Q_i then dO_i
     static constexpr int kQ = kOnes + 1024;                         // [kStages] at stride kStageBytes
     static constexpr int kDo = kQ + kTileBytes;                     // [kStages] at stride kStageBytes
     static constexpr int kExt = kQ + kStages * kStageBytes;         // [kStages] per-query rows
-    static constexpr int kStg = kExt + kStages * kExtTileBytes;     // dQ staging: 128 rows x 32 floats
-    static constexpr int kDs = kStg + 16384;                        // dS^T: 2 atoms x 128 rows x 128 bytes
+    static constexpr int kStg = kExt + kStages * kExtTileBytes;     // dQ staging, two buffers of 128 rows x 32 floats
+    static constexpr int kDs = kStg + 2 * 16384;                    // dS^T: 2 atoms x 128 rows x 128 bytes
     static constexpr int kLse = kDs + 32768;                        // [softmax warps][32] float
-    static constexpr int kBars = kLse + kSoftmaxWarps * 128;
-    static constexpr int kMisc = kBars + kNumBarriers * 8;
+    static constexpr int kItems = kLse + kSoftmaxWarps * 128;       // [2] Item
+    static constexpr int kBars = kItems + 2 * 32;
+    static constexpr int kMisc = kBars + (kNumBarriers + 1) / 2 * 16;
     static constexpr int kDynamic = kMisc + 16 + 1024;              // slack for the 1024-byte alignment
-    static_assert(kOnes % 1024 == 0 && kQ % 1024 == 0 && kExt % 1024 == 0 && kStg % 1024 == 0 && kDs % 1024 == 0 && kLse % 16 == 0 && kBars % 8 == 0, "aligned");
+    static_assert(kOnes % 1024 == 0 && kQ % 1024 == 0 && kExt % 1024 == 0 && kStg % 1024 == 0 && kDs % 1024 == 0 && kLse % 16 == 0 &&
+                  kItems % 16 == 0 && kBars % 16 == 0 && kMisc % 16 == 0 && kDynamic <= 227 * 1024, "aligned, and within an SM");
+};
+
+struct alignas(16) Item {
+    int32_t node0, n, head, kv0;           // n = 0: there are no more
+    int32_t prefix, q_lo, pad[2];          // q_lo: first query that sees a key of the tile, in whole tiles
+    __device__ __forceinline__ int32_t q_tiles() const { return (n - q_lo + kTile - 1) / kTile; }
+    // rows of the last query tile that are the document's, if rows of another one follow in it, else 0
+    __device__ __forceinline__ int32_t ragged(int32_t n_total) const { return node0 + n < n_total ? n % kTile : 0; }
 };
 
 // register budget: the CTA is launched with 768 x 80 registers; after the re-split it holds
-// 128 x 40 + 512 x 96 + 128 x 48 = 60416 <= 61440 (an increase can only draw on what the CTA owns)
+// 128 x 48 + 512 x 96 + 128 x 48 = 61440 (an increase can only draw on what the CTA owns)
 __device__ __forceinline__ void setmaxnreg_inc_96() { asm volatile("setmaxnreg.inc.sync.aligned.u32 96;"); }
 __device__ __forceinline__ void setmaxnreg_dec_48() { asm volatile("setmaxnreg.dec.sync.aligned.u32 48;"); }
 
@@ -117,32 +139,18 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    int h = blockIdx.x, g = blockIdx.z, kv_tile = blockIdx.y;
-    int32_t node0 = 0, n = p.n_total;
-    if (p.cu_seqlens) grid_wait();          // a single document's blocks set up their barriers and tensor memory before they wait
-    if (p.list) {
-        const int4 entry = p.list[blockIdx.x / (unsigned)p.n_heads];
-        if (entry.x < 0) return;
-        h = (int)(blockIdx.x % (unsigned)p.n_heads);
-        g = entry.x;
-        kv_tile = entry.y;
-        node0 = entry.z;
-        n = entry.w;
-    } else if (p.cu_seqlens) {
-        node0 = p.cu_seqlens[g];
-        n = p.cu_seqlens[g + 1] - node0;
-    }
-    const int32_t kv0 = kv_tile * kTile;
-    if (kv0 >= n) return;
-
     uint64_t* bars = (uint64_t*)(smem + L::kBars);
     uint32_t* misc = (uint32_t*)(smem + L::kMisc);
+    Item* items = (Item*)(smem + L::kItems);
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     volatile uint32_t* abort_flag = &misc[1];
     if (tid == 0) {
         misc[1] = 0u;
-        mbar_init(bar(kBarKvFull), 1);
         for (int s = 0; s < 2; ++s) {
+            mbar_init(bar(kBarItemFull + s), 1);
+            mbar_init(bar(kBarItemEmpty + s), 3 + kSoftmaxWarps + 4);
+            mbar_init(bar(kBarKFull + s), 1);
+            mbar_init(bar(kBarKEmpty + s), 1);
             mbar_init(bar(kBarQdoFull + s), 1);
             mbar_init(bar(kBarStageEmpty + s), 2);
             mbar_init(bar(kBarSFull + s), 1);
@@ -150,37 +158,23 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             mbar_init(bar(kBarPReady + s), kSoftmaxWarps / 2);       // one arrival per warp
             mbar_init(bar(kBarDsReady + s), kSoftmaxWarps / 2);
         }
+        mbar_init(bar(kBarVFull), 1);
+        mbar_init(bar(kBarVEmpty), 4);
         mbar_init(bar(kBarDqFull), 1);
         mbar_init(bar(kBarDqFree), 4);
         mbar_init(bar(kBarKvTmem), 8);
-        mbar_init(bar(kBarKClear), 1);
         mbar_init(bar(kBarQClear), 1);
-        mbar_init(bar(kBarFinal), 3);
+        mbar_init(bar(kBarFinal), 2);
+        mbar_init(bar(kBarAccFree), kSoftmaxWarps);
         fence_mbar_init();
+        prefetch_tensormap(&tmap_q);
+        prefetch_tensormap(&tmap_k);
+        prefetch_tensormap(&tmap_v);
+        prefetch_tensormap(&tmap_do);
+        prefetch_tensormap(&tmap_ext);
+        prefetch_tensormap(&tmap_dq);
     }
     if (warp == 2) { tmem_alloc(smem_u32(&misc[0]), 512); tmem_relinquish(); }
-    if (!p.cu_seqlens) grid_wait();
-    const int32_t prefix = p.prefix ? p.prefix[g] : 0;
-    const int32_t q_lo = p.causal && kv0 >= prefix ? kv0 : 0;              // first query that sees a key of the tile, in whole tiles
-    const int32_t n_q = (n - q_lo + kTile - 1) / kTile;
-    const bool others_behind = node0 + n < p.n_total;
-    const bool k_ragged = others_behind && kv0 + kTile > n, q_ragged = others_behind && n % kTile != 0;
-    const int kv_head = h / p.group;
-    auto load_q_do = [&](int i) {
-        const int s = i & 1;
-        const int32_t row = node0 + q_lo + i * kTile;
-        mbar_arrive_expect_tx(bar(kBarQdoFull + s), 2 * L::kTileBytes + kExtTileBytes);
-        tma_load_3d(smem_u32(smem + L::kQ + s * L::kStageBytes), &tmap_q, bar(kBarQdoFull + s), 0, h, row);
-        tma_load_3d(smem_u32(smem + L::kDo + s * L::kStageBytes), &tmap_do, bar(kBarQdoFull + s), 0, h, row);
-        tma_load_3d(smem_u32(smem + L::kExt + s * kExtTileBytes), &tmap_ext, bar(kBarQdoFull + s), 0, h, row);
-    };
-    if (tid == 0) {                          // the first tiles are on their way while the block is still setting up
-        mbar_arrive_expect_tx(bar(kBarKvFull), 2 * L::kTileBytes);
-        tma_load_3d(smem_u32(smem + L::kK), &tmap_k, bar(kBarKvFull), 0, kv_head, node0 + kv0);
-        tma_load_3d(smem_u32(smem + L::kV), &tmap_v, bar(kBarKvFull), 0, kv_head, node0 + kv0);
-        load_q_do(0);
-    }
-    if (p.early_release) grid_release();
     if (tid < 32) {
         // 8 rows x 32 bytes per group in the 32-byte swizzle: the 16-byte half that holds columns 0..7 sits
         // first in rows 0-3 and second in rows 4-7.  Group 0: ones in columns 0..2 (multiplies the -lse terms),
@@ -195,32 +189,95 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = misc[0];
+    grid_wait();
+    if (p.early_release) grid_release();
     constexpr uint32_t kColDv = 256, kColDk = 320, kColDq = 384, kColK = 448, kColV = 480;
 
+    // Item number k of this CTA; false: there are no more.  give_back: the calling warp is done with its description.
+    auto take = [&](int k) -> bool {
+        mbar_wait(bar(kBarItemFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 300);
+        return items[k & 1].n > 0 && *abort_flag == 0u;
+    };
+    auto give_back = [&](int k) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(kBarItemEmpty + (k & 1)));
+    };
+
     if (warp < 4) {
-        setmaxnreg_dec_40();
+        setmaxnreg_dec_48();
         if (warp == 0) {
-            // ------------------------------ TMA producer ------------------------------
-            if (k_ragged) {
-                mbar_wait(bar(kBarKvFull), 0, abort_flag, p.status, 309);
-                clear_rows(smem + L::kK, n - kv0, L::kRowBytes);
-                fence_proxy_async_smem();
+            // ------------------------------ items and TMA producer ------------------------------
+            // The CTA's own number, then what the counter gives, as late as can be: when the last rows of the item before are on their way.
+            int32_t index = (int32_t)blockIdx.x;
+            int c = 0;                                       // query tiles so far
+            for (int k = 0;; ++k) {
+                Item item{};
+                while (item.n == 0) {
+                    if (index < 0) {
+                        uint32_t taken = (uint32_t)p.n_items;
+                        if (lane == 0 && (int32_t)gridDim.x < p.n_items) {
+                            taken = atomicAdd(p.next_item, 1u);
+                            // every item beyond the first ones is counted once, and every CTA's vain attempt: the last one leaves 0
+                            if (taken == (uint32_t)p.n_items - 1u) *p.next_item = 0u;
+                        }
+                        index = (int32_t)(gridDim.x + __shfl_sync(0xffffffffu, taken, 0));
+                    }
+                    if (index >= p.n_items) break;
+                    int32_t g, tile;
+                    if (p.list) {
+                        const int4 entry = p.list[index / p.n_heads];
+                        g = entry.x;
+                        tile = entry.y;
+                        item.node0 = entry.z;
+                        item.n = entry.x < 0 ? 0 : entry.w;
+                    } else {
+                        const int32_t row = index / p.n_heads;
+                        tile = row / p.n_graphs;
+                        g = row % p.n_graphs;
+                        item.node0 = p.cu_seqlens ? p.cu_seqlens[g] : 0;
+                        item.n = p.cu_seqlens ? p.cu_seqlens[g + 1] - item.node0 : p.n_total;
+                    }
+                    item.head = index % p.n_heads;
+                    index = -1;
+                    item.kv0 = tile * kTile;
+                    if (item.kv0 >= item.n) {
+                        item.n = 0;
+                    } else {
+                        item.prefix = p.prefix ? p.prefix[g] : 0;
+                        item.q_lo = p.causal && item.kv0 >= item.prefix ? item.kv0 : 0;
+                    }
+                }
+                if (k >= 2) mbar_wait(bar(kBarItemEmpty + (k & 1)), ((k >> 1) & 1) ^ 1, abort_flag, p.status, 301);
+                if (lane == 0) {
+                    items[k & 1] = item;
+                    mbar_arrive(bar(kBarItemFull + (k & 1)));
+                }
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(kBarKClear));
-            }
-            for (int i = 1; i < n_q; ++i) {
-                mbar_wait(bar(kBarStageEmpty + (i & 1)), ((i >> 1) & 1) ^ 1, abort_flag, p.status, 310);
-                if (lane == 0) load_q_do(i);
-                __syncwarp();
-            }
-            if (q_ragged) {                          // (the last tile's own phase: nothing is loaded behind it)
-                const int s = (n_q - 1) & 1, first = n - q_lo - (n_q - 1) * kTile;
-                mbar_wait(bar(kBarQdoFull + s), ((n_q - 1) >> 1) & 1, abort_flag, p.status, 311);
-                clear_rows(smem + L::kQ + s * L::kStageBytes, first, L::kRowBytes);
-                clear_rows(smem + L::kDo + s * L::kStageBytes, first, L::kRowBytes);
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(kBarQClear));
+                if (item.n == 0) break;
+                const int kv_head = item.head / p.group;
+                if (k >= 2) mbar_wait(bar(kBarKEmpty + (k & 1)), ((k >> 1) & 1) ^ 1, abort_flag, p.status, 302);
+                if (lane == 0) {
+                    mbar_arrive_expect_tx(bar(kBarKFull + (k & 1)), L::kTileBytes);
+                    tma_load_3d(smem_u32(smem + L::kK + (k & 1) * L::kTileBytes), &tmap_k, bar(kBarKFull + (k & 1)), 0, kv_head, item.node0 + item.kv0);
+                }
+                if (k >= 1) mbar_wait(bar(kBarVEmpty), (k - 1) & 1, abort_flag, p.status, 303);
+                if (lane == 0) {
+                    mbar_arrive_expect_tx(bar(kBarVFull), L::kTileBytes);
+                    tma_load_3d(smem_u32(smem + L::kV), &tmap_v, bar(kBarVFull), 0, kv_head, item.node0 + item.kv0);
+                }
+                const int n_q = item.q_tiles();
+                for (int i = 0; i < n_q; ++i, ++c) {
+                    const int s = c & 1;
+                    if (c >= 2) mbar_wait(bar(kBarStageEmpty + s), ((c >> 1) & 1) ^ 1, abort_flag, p.status, 310);
+                    if (lane == 0) {
+                        const int32_t row = item.node0 + item.q_lo + i * kTile;
+                        mbar_arrive_expect_tx(bar(kBarQdoFull + s), 2 * L::kTileBytes + kExtTileBytes);
+                        tma_load_3d(smem_u32(smem + L::kQ + s * L::kStageBytes), &tmap_q, bar(kBarQdoFull + s), 0, item.head, row);
+                        tma_load_3d(smem_u32(smem + L::kDo + s * L::kStageBytes), &tmap_do, bar(kBarQdoFull + s), 0, item.head, row);
+                        tma_load_3d(smem_u32(smem + L::kExt + s * kExtTileBytes), &tmap_ext, bar(kBarQdoFull + s), 0, item.head, row);
+                    }
+                    __syncwarp();
+                }
             }
         } else if (warp == 1 || warp == 3) {
             // ------------------------------- MMA issuers -------------------------------
@@ -238,8 +295,8 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             const uint32_t reg_off = on_p ? 0 : kHalf;          // S^T/P^T or dP^T/dS^T part of a TMEM stage
             const uint32_t in_a_col = on_p ? kColK : kColV;
             const int bar_ready = on_p ? kBarPReady : kBarDsReady, bar_full = on_p ? kBarSFull : kBarDpFull;
-            auto issue_input = [&](int i, int sub) {            // (S^T - lse sqrt(d)) or (dP^T - Delta) of a half tile
-                const int s = i & 1;
+            auto issue_input = [&](int c, int sub) {            // (S^T - lse sqrt(d)) or (dP^T - Delta) of a half tile
+                const int s = c & 1;
                 const uint64_t db = make_smem_desc(smem_u32(smem + in_b_off + s * L::kStageBytes) + sub * kHalf * L::kRowBytes, L::kRowBytes, 0);
                 const uint64_t dext = make_smem_desc(smem_u32(smem + L::kExt + s * kExtTileBytes) + sub * kHalf * kExtCols * 2, kExtCols * 2, 0);
                 const uint32_t d = tm + sub * 128 + reg_off;
@@ -249,62 +306,90 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 if (!kCap || !on_p) mma_ss(d, desc_ones, dext, idesc_in, 1u);
                 mma_commit(bar(bar_full + sub));
             };
-            auto wait_tile = [&](int i) {
-                mbar_wait(bar(kBarQdoFull + (i & 1)), (i >> 1) & 1, abort_flag, p.status, 321);
-                if (q_ragged && i == n_q - 1) mbar_wait(bar(kBarQClear), 0, abort_flag, p.status, 322);
-            };
-            mbar_wait(bar(kBarKvTmem), 0, abort_flag, p.status, 320);
-            wait_tile(0);
-            tc_fence_after();
-            if (elect_one()) { issue_input(0, 0); issue_input(0, 1); }
-            __syncwarp();
-            bool acc_started = false;           // the first MMA into the accumulator overwrites it
-            for (int i = 0; i < n_q; ++i) {
-                const int s = i & 1;
-                if (i + 1 < n_q) wait_tile(i + 1);
+            int c = 0, cleared = 0;                             // query tiles, and ragged ones, so far
+            for (int k = 0; take(k); ++k) {
+                const int n_q = items[k & 1].q_tiles();
+                const bool ragged = items[k & 1].ragged(p.n_total) != 0;
+                give_back(k);
+                auto wait_tile = [&](int i) {
+                    mbar_wait(bar(kBarQdoFull + ((c + i) & 1)), ((c + i) >> 1) & 1, abort_flag, p.status, 321);
+                    if (ragged && i == n_q - 1) mbar_wait(bar(kBarQClear), cleared & 1, abort_flag, p.status, 322);
+                };
+                mbar_wait(bar(kBarKvTmem), k & 1, abort_flag, p.status, 320);
+                wait_tile(0);
+                tc_fence_after();
+                if (elect_one()) { issue_input(c, 0); issue_input(c, 1); }
+                __syncwarp();
+                if (k > 0) mbar_wait(bar(kBarAccFree), (k - 1) & 1, abort_flag, p.status, 324);
+                bool acc_started = false;           // the first MMA into the accumulator overwrites it
+                for (int i = 0; i < n_q; ++i) {
+                    const int s = (c + i) & 1;
+                    if (i + 1 < n_q) wait_tile(i + 1);
 #pragma unroll
-                for (int sub = 0; sub < 2; ++sub) {
-                    mbar_wait(bar(bar_ready + sub), i & 1, abort_flag, p.status, 323);
-                    tc_fence_after();
-                    if (elect_one()) {
-                        const uint32_t t_a = tm + sub * 128 + reg_off;
-                        const uint64_t db = make_smem_desc(smem_u32(smem + acc_b_off + s * L::kStageBytes) + sub * kHalf * L::kRowBytes, L::kRowBytes, 0);
+                    for (int sub = 0; sub < 2; ++sub) {
+                        mbar_wait(bar(bar_ready + sub), (c + i) & 1, abort_flag, p.status, 323);
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const uint32_t t_a = tm + sub * 128 + reg_off;
+                            const uint64_t db = make_smem_desc(smem_u32(smem + acc_b_off + s * L::kStageBytes) + sub * kHalf * L::kRowBytes, L::kRowBytes, 0);
 #pragma unroll
-                        for (int ks = 0; ks < kHalf / 16; ++ks)     // A: bf16 pairs of query group ks/2 at the start of its 32 columns
-                            mma_ts(tm + acc_col, t_a + (ks >> 1) * 32 + (ks & 1) * 8,
-                                   advance_desc(db, ks * 16 * L::kRowBytes), idesc_ts, (acc_started || ks > 0) ? 1u : 0u);
-                        if (sub == 1) {
-                            mma_commit(bar(kBarStageEmpty + s));    // this issuer's reads of Q_i / dO_i are done (the other one commits too)
-                            if (i + 1 == n_q) mma_commit(bar(kBarFinal));
+                            for (int ks = 0; ks < kHalf / 16; ++ks)     // A: bf16 pairs of query group ks/2 at the start of its 32 columns
+                                mma_ts(tm + acc_col, t_a + (ks >> 1) * 32 + (ks & 1) * 8,
+                                       advance_desc(db, ks * 16 * L::kRowBytes), idesc_ts, (acc_started || ks > 0) ? 1u : 0u);
+                            if (sub == 1) {
+                                mma_commit(bar(kBarStageEmpty + s));    // this issuer's reads of Q_i / dO_i are done (the other one commits too)
+                                if (i + 1 == n_q) mma_commit(bar(kBarFinal));
+                            }
+                            if (i + 1 < n_q) issue_input(c + i + 1, sub);
                         }
-                        if (i + 1 < n_q) issue_input(i + 1, sub);
+                        __syncwarp();
+                        acc_started = true;
                     }
-                    __syncwarp();
-                    acc_started = true;
                 }
+                c += n_q;
+                cleared += ragged ? 1 : 0;
             }
-        } else if (warp == 2) {
-            // ------------------------------- dQ issuer -------------------------------
+        } else {
+            // ------------------- dQ issuer; clears what lies behind the document in K, Q and dO -------------------
             constexpr uint32_t idesc_dq = make_idesc_bf16(128, D, true, true);         // A and B MN-major
             const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
-            const uint64_t desc_k = make_smem_desc(smem_u32(smem + L::kK), L::kRowBytes, 0);
             const uint64_t da = make_smem_desc(smem_u32(smem + L::kDs), 128, 16384);
-            mbar_wait(bar(kBarKvFull), 0, abort_flag, p.status, 330);
-            if (k_ragged) mbar_wait(bar(kBarKClear), 0, abort_flag, p.status, 331);
-            for (int i = 0; i < n_q; ++i) {
-                // dQ_i = dS K once both halves have stored dS^T(i) and the reducer has drained dQ_{i-1}
-                mbar_wait(bar(kBarDsReady + 0), i & 1, abort_flag, p.status, 332);
-                mbar_wait(bar(kBarDsReady + 1), i & 1, abort_flag, p.status, 333);
-                mbar_wait(bar(kBarDqFree), (i & 1) ^ 1, abort_flag, p.status, 334);
-                tc_fence_after();
-                if (elect_one()) {
-#pragma unroll
-                    for (int ks = 0; ks < 8; ++ks)
-                        mma_ss(tm + kColDq, advance_desc(da, ks * 2048), advance_desc(desc_k, ks * 16 * L::kRowBytes), idesc_dq, ks > 0);
-                    mma_commit(bar(kBarDqFull));
-                    if (i + 1 == n_q) mma_commit(bar(kBarFinal));
-                }
+            int c = 0;
+            for (int k = 0; take(k); ++k) {
+                const int n_q = items[k & 1].q_tiles();
+                const int q_rows = items[k & 1].ragged(p.n_total), k_rows = q_rows != 0 ? items[k & 1].n - items[k & 1].kv0 : kTile;
+                give_back(k);
+                uint8_t* const s_k = smem + L::kK + (k & 1) * L::kTileBytes;
+                const uint64_t desc_k = make_smem_desc(smem_u32(s_k), L::kRowBytes, 0);
+                mbar_wait(bar(kBarKFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 330);
+                if (k_rows < kTile) clear_rows(s_k, k_rows, L::kRowBytes);
+                auto clear_tile = [&](int at) {                // tile number `at`, the item's last one, before any MMA reads it
+                    mbar_wait(bar(kBarQdoFull + (at & 1)), (at >> 1) & 1, abort_flag, p.status, 331);
+                    clear_rows(smem + L::kQ + (at & 1) * L::kStageBytes, q_rows, L::kRowBytes);
+                    clear_rows(smem + L::kDo + (at & 1) * L::kStageBytes, q_rows, L::kRowBytes);
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(kBarQClear));
+                };
+                fence_proxy_async_smem();
                 __syncwarp();
+                if (q_rows != 0 && n_q == 1) clear_tile(c);
+                for (int i = 0; i < n_q; ++i, ++c) {
+                    if (q_rows != 0 && i == n_q - 2) clear_tile(c + 1);
+                    // dQ_i = dS K once both halves have stored dS^T(i) and the reducer has drained dQ_{i-1}
+                    mbar_wait(bar(kBarDsReady + 0), c & 1, abort_flag, p.status, 332);
+                    mbar_wait(bar(kBarDsReady + 1), c & 1, abort_flag, p.status, 333);
+                    mbar_wait(bar(kBarDqFree), (c & 1) ^ 1, abort_flag, p.status, 334);
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int ks = 0; ks < 8; ++ks)
+                            mma_ss(tm + kColDq, advance_desc(da, ks * 2048), advance_desc(desc_k, ks * 16 * L::kRowBytes), idesc_dq, ks > 0);
+                        mma_commit(bar(kBarDqFull));
+                        if (i + 1 == n_q) mma_commit(bar(kBarKEmpty + (k & 1)));
+                    }
+                    __syncwarp();
+                }
             }
         }
     } else if (warp < 20) {
@@ -316,42 +401,58 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t tS = tmem + half * 128 + (grp & 1) * 32 + lane_off;
         const uint32_t tDp = tS + kHalf;
-        const int32_t key = kv0 + r, key0 = kv0 + (warp & 3) * 32;               // this thread's key, the warp's first one
-        // queries [from, to) see the key
-        const int32_t from = p.causal && key >= prefix ? key : 0, to = key < n ? n : 0;
-        const int32_t last_from = p.causal && key0 + 31 >= prefix ? key0 + 31 : 0;               // largest `from` of the warp
         const uint64_t c1c1 = both(p.c1);
         [[maybe_unused]] const uint64_t to_tanh2 = both(p.to_tanh), cap22 = both(p.cap2);
-        [[maybe_unused]] const float slope2 = kSlope ? p.slopes[h] * kLog2e : 0.f;
         [[maybe_unused]] float* s_lse = (float*)(smem + L::kLse) + (warp - 4) * 32;
-        // lse of the warp's queries, a lane each, fetched a tile ahead
-        [[maybe_unused]] auto fetch_lse = [&](int i) -> float {
-            const int32_t q = q_lo + i * kTile + grp * 32 + lane;
-            return q < n ? -kLog2e * p.lse[(size_t)h * p.n_total + node0 + q] : 0.f;
-        };
-        [[maybe_unused]] float next_lse = kCap ? fetch_lse(0) : 0.f;
         uint8_t* ds_row = smem + L::kDs + half * 16384 + r * 128;
 
-        // K (warps 4-7) and V (warps 8-11) rows -> tensor memory, where they stay as the A operands of S^T = K Q^T and dP^T = V dO^T
-        if (warp < 12) {
-            mbar_wait(bar(kBarKvFull), 0, abort_flag, p.status, 344);
-            const uint8_t* src = smem + (warp < 8 ? L::kK : L::kV) + r * L::kRowBytes;
+        // K (warps 4-7) and V (warps 8-11) rows of item k -> tensor memory, where they stay as the A operands of S^T = K Q^T and
+        // dP^T = V dO^T, once all MMAs that read the last item's there are done (c: query tiles so far; both halves of the last one)
+        auto copy_kv = [&](int k, int c) {
+            if (warp >= 12) return;
+            if (c > 0) mbar_wait(bar((warp < 8 ? kBarSFull : kBarDpFull) + 1), (c - 1) & 1, abort_flag, p.status, 345);
+            if (warp < 8) mbar_wait(bar(kBarKFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 344);
+            else mbar_wait(bar(kBarVFull), k & 1, abort_flag, p.status, 346);
+            tc_fence_after();
+            const uint8_t* src = smem + (warp < 8 ? L::kK + (k & 1) * L::kTileBytes : L::kV) + r * L::kRowBytes;
             uint32_t w[D / 2];
 #pragma unroll
-            for (int c = 0; c < D / 8; ++c) {
-                const int phys = D == 64 ? (c ^ (r & 7)) : (c ^ ((r >> 1) & 3));     // 128-byte / 64-byte swizzle
+            for (int e = 0; e < D / 8; ++e) {
+                const int phys = D == 64 ? (e ^ (r & 7)) : (e ^ ((r >> 1) & 3));     // 128-byte / 64-byte swizzle
                 const uint4 v4 = *(const uint4*)(src + (phys << 4));
-                w[4 * c] = v4.x; w[4 * c + 1] = v4.y; w[4 * c + 2] = v4.z; w[4 * c + 3] = v4.w;
+                w[4 * e] = v4.x; w[4 * e + 1] = v4.y; w[4 * e + 2] = v4.z; w[4 * e + 3] = v4.w;
             }
             const uint32_t dst = tmem + (warp < 8 ? kColK : kColV) + lane_off;
             if constexpr (D == 64) tmem_st32(dst, w); else tmem_st16(dst, w);
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar(kBarKvTmem));
-        }
+            if (lane == 0) {
+                if (warp >= 8) mbar_arrive(bar(kBarVEmpty));
+                mbar_arrive(bar(kBarKvTmem));
+            }
+        };
 
-        for (int i = 0; i < n_q; ++i) {
+        int c = 0;                                      // query tiles so far
+        if (take(0)) copy_kv(0, 0);
+        for (int k = 0; items[k & 1].n > 0 && *abort_flag == 0u; ++k) {
+        const int32_t n = items[k & 1].n, q_lo = items[k & 1].q_lo;
+        const int32_t key = items[k & 1].kv0 + r, key0 = key - lane;                        // this thread's key, the warp's first one
+        // queries [from, to) see the key
+        [[maybe_unused]] const int32_t prefix = items[k & 1].prefix;
+        const int32_t from = p.causal && key >= prefix ? key : 0, to = key < n ? n : 0;
+        const int32_t last_from = p.causal && key0 + 31 >= prefix ? key0 + 31 : 0;               // largest `from` of the warp
+        [[maybe_unused]] const float slope2 = kSlope ? p.slopes[items[k & 1].head] * kLog2e : 0.f;
+        // lse of the warp's queries, a lane each, fetched a tile ahead
+        [[maybe_unused]] const float* lse_row = p.lse + (size_t)items[k & 1].head * p.n_total + items[k & 1].node0;
+        [[maybe_unused]] auto fetch_lse = [&](int i) -> float {
+            const int32_t q = q_lo + i * kTile + grp * 32 + lane;
+            return q < n ? -kLog2e * lse_row[q] : 0.f;
+        };
+        [[maybe_unused]] float next_lse = kCap ? fetch_lse(0) : 0.f;
+        const int n_q = items[k & 1].q_tiles();
+
+        for (int i = 0; i < n_q; ++i, ++c) {
             const int32_t q0 = q_lo + i * kTile + grp * 32;                     // the group's first query
             const bool masked = q0 < last_from || q0 + 32 > n || key0 + 32 > n;     // some pair of the warp's may not count
             const int c_from = from - q0, c_to = to - q0;
@@ -368,7 +469,7 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             }
             float pr[32];                            // P^T, then dS^T (capped scores: P^T (1 - tanh^2) in between)
             uint32_t pk[16];
-            mbar_wait(bar(kBarSFull + half), i & 1, abort_flag, p.status, 340);
+            mbar_wait(bar(kBarSFull + half), c & 1, abort_flag, p.status, 340);
             tc_fence_after();
 
             // ---------------- P^T = exp2((S^T - lse sqrt(d)) c1), or exp2(cap log2(e) tanh(S^T / cap) - lse log2(e)) ----------------
@@ -378,17 +479,17 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 tmem_ld32(tS, sv);
                 tmem_wait_ld();
 #pragma unroll
-                for (int c = 0; c < 32; c += 2) {
+                for (int e = 0; e < 32; e += 2) {
                     uint64_t add = both(0.f), x;
                     if constexpr (kCap) {
-                        const float2 nl = *(const float2*)(s_lse + c);
+                        const float2 nl = *(const float2*)(s_lse + e);
                         add = pack_f32x2(nl.x, nl.y);
                     }
                     if constexpr (kSlope) {
-                        if constexpr (decltype(general)::value) add = add_f32x2(add, pack_f32x2(-slope2 * fabsf((float)(q0 + c - key)), -slope2 * fabsf((float)(q0 + c + 1 - key))));
-                        else add = fma_f32x2(both(step_slope), pack_f32x2((float)(q0 + c - key), (float)(q0 + c + 1 - key)), add);
+                        if constexpr (decltype(general)::value) add = add_f32x2(add, pack_f32x2(-slope2 * fabsf((float)(q0 + e - key)), -slope2 * fabsf((float)(q0 + e + 1 - key))));
+                        else add = fma_f32x2(both(step_slope), pack_f32x2((float)(q0 + e - key), (float)(q0 + e + 1 - key)), add);
                     }
-                    const uint64_t raw = pack_u32x2(sv[c], sv[c + 1]);
+                    const uint64_t raw = pack_u32x2(sv[e], sv[e + 1]);
                     [[maybe_unused]] uint64_t t;
                     if constexpr (kCap) {
                         const uint64_t u = mul_f32x2(raw, to_tanh2);
@@ -414,16 +515,16 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     lo = ex2_approx(lo);
                     hi = ex2_approx(hi);
                     if constexpr (decltype(masked_)::value) {
-                        if (c < c_from || c >= c_to) lo = 0.f;
-                        if (c + 1 < c_from || c + 1 >= c_to) hi = 0.f;
+                        if (e < c_from || e >= c_to) lo = 0.f;
+                        if (e + 1 < c_from || e + 1 >= c_to) hi = 0.f;
                     }
-                    pk[c >> 1] = pack_bf16x2(lo, hi);
+                    pk[e >> 1] = pack_bf16x2(lo, hi);
                     if constexpr (kCap) {
                         const uint64_t minus = mul_f32x2(t, both(-1.f));
-                        unpack_f32x2(mul_f32x2(pack_f32x2(lo, hi), fma_f32x2(minus, t, both(1.f))), pr[c], pr[c + 1]);
+                        unpack_f32x2(mul_f32x2(pack_f32x2(lo, hi), fma_f32x2(minus, t, both(1.f))), pr[e], pr[e + 1]);
                     } else {
-                        pr[c] = lo;
-                        pr[c + 1] = hi;
+                        pr[e] = lo;
+                        pr[e + 1] = hi;
                     }
                 }
             };
@@ -436,7 +537,7 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             }
             tmem_st16(tS, pk);                      // P^T of this group: 16 packed columns at the start of its range
             uint32_t dpa[16], dpb[16];
-            mbar_wait(bar(kBarDpFull + half), i & 1, abort_flag, p.status, 341);
+            mbar_wait(bar(kBarDpFull + half), c & 1, abort_flag, p.status, 341);
             tc_fence_after();
             tmem_ld16(tDp, dpa);
             tmem_ld16(tDp + 16, dpb);
@@ -450,14 +551,14 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             auto ds_round = [&](int rnd, const uint32_t (&dp)[16], auto masked_) {
 #pragma unroll
                 for (int k = 0; k < 16; k += 2) {
-                    const int c = rnd * 16 + k;
+                    const int e = rnd * 16 + k;
                     float lo, hi;
-                    unpack_f32x2(mul_f32x2(pack_f32x2(pr[c], pr[c + 1]), pack_u32x2(dp[k], dp[k + 1])), lo, hi);
+                    unpack_f32x2(mul_f32x2(pack_f32x2(pr[e], pr[e + 1]), pack_u32x2(dp[k], dp[k + 1])), lo, hi);
                     if constexpr (decltype(masked_)::value) {      // (0 x NaN: a row of V that is another document's, or of this one's queries that do not see the key)
-                        if (c < c_from || c >= c_to) lo = 0.f;
-                        if (c + 1 < c_from || c + 1 >= c_to) hi = 0.f;
+                        if (e < c_from || e >= c_to) lo = 0.f;
+                        if (e + 1 < c_from || e + 1 >= c_to) hi = 0.f;
                     }
-                    pk[c >> 1] = pack_bf16x2(lo, hi);
+                    pk[e >> 1] = pack_bf16x2(lo, hi);
                 }
             };
             if (masked) {
@@ -469,7 +570,7 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             }
             tmem_st16(tDp, pk);
             // dQ of the previous tile has read the dS^T tile in shared memory
-            if (i > 0) mbar_wait(bar(kBarDqFull), (i - 1) & 1, abort_flag, p.status, 342);
+            if (c > 0) mbar_wait(bar(kBarDqFull), (c - 1) & 1, abort_flag, p.status, 342);
 #pragma unroll
             for (int c8 = 0; c8 < 4; ++c8)
                 *(uint4*)(ds_row + ((((grp & 1) * 4 + c8) ^ (r & 7)) << 4)) = make_uint4(pk[4 * c8], pk[4 * c8 + 1], pk[4 * c8 + 2], pk[4 * c8 + 3]);
@@ -480,8 +581,9 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             if (lane == 0) mbar_arrive(bar(kBarDsReady + half));
         }
 
-        // ---------------- epilogue: dV (first half's warps) and dK (second half's) ----------------
-        mbar_wait(bar(kBarFinal), 0, abort_flag, p.status, 343);
+        // ---------------- the next item's K and V, then dV (first half's warps) and dK (second half's) ----------------
+        if (take(k + 1)) copy_kv(k + 1, c);
+        mbar_wait(bar(kBarFinal), k & 1, abort_flag, p.status, 343);
         tc_fence_after();
         constexpr int kOC = D / 2;                  // output columns per thread
         const int ch = grp & 1;
@@ -489,63 +591,72 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         uint32_t o[kOC];
         if constexpr (kOC == 32) tmem_ld32(tacc, o); else tmem_ld16(tacc, o);
         tmem_wait_ld();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(kBarAccFree));
         if (key < n) {
+            const int32_t node = items[k & 1].node0 + key, kv_head = items[k & 1].head / p.group;
             if (p.dk_acc != nullptr) {
-                const size_t at = ((size_t)(node0 + key) * (p.n_heads / p.group) + kv_head) * D + ch * kOC;
+                const size_t at = ((size_t)node * (p.n_heads / p.group) + kv_head) * D + ch * kOC;
                 float4* dst = (float4*)((half == 0 ? p.dv_acc : p.dk_acc) + at);
 #pragma unroll
-                for (int k = 0; k < kOC / 4; ++k) red_add_f32x4(dst + k, o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+                for (int e = 0; e < kOC / 4; ++e) red_add_f32x4(dst + e, o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
             } else {
                 const float mul = half == 0 ? 1.0f : p.scale;
-                __nv_bfloat16* row = half == 0 ? p.dv + (int64_t)(node0 + key) * p.dv_row : p.dk + (int64_t)(node0 + key) * p.dk_row;
-                uint4* dst = (uint4*)(row + h * D + ch * kOC);
+                __nv_bfloat16* row = half == 0 ? p.dv + (int64_t)node * p.dv_row : p.dk + (int64_t)node * p.dk_row;
+                uint4* dst = (uint4*)(row + kv_head * D + ch * kOC);
 #pragma unroll
-                for (int k = 0; k < kOC / 8; ++k) {
+                for (int e = 0; e < kOC / 8; ++e) {
                     uint4 v;
-                    v.x = pack_bf16x2(__uint_as_float(o[8 * k]) * mul, __uint_as_float(o[8 * k + 1]) * mul);
-                    v.y = pack_bf16x2(__uint_as_float(o[8 * k + 2]) * mul, __uint_as_float(o[8 * k + 3]) * mul);
-                    v.z = pack_bf16x2(__uint_as_float(o[8 * k + 4]) * mul, __uint_as_float(o[8 * k + 5]) * mul);
-                    v.w = pack_bf16x2(__uint_as_float(o[8 * k + 6]) * mul, __uint_as_float(o[8 * k + 7]) * mul);
-                    dst[k] = v;
+                    v.x = pack_bf16x2(__uint_as_float(o[8 * e]) * mul, __uint_as_float(o[8 * e + 1]) * mul);
+                    v.y = pack_bf16x2(__uint_as_float(o[8 * e + 2]) * mul, __uint_as_float(o[8 * e + 3]) * mul);
+                    v.z = pack_bf16x2(__uint_as_float(o[8 * e + 4]) * mul, __uint_as_float(o[8 * e + 5]) * mul);
+                    v.w = pack_bf16x2(__uint_as_float(o[8 * e + 6]) * mul, __uint_as_float(o[8 * e + 7]) * mul);
+                    dst[e] = v;
                 }
             }
         }
+        give_back(k);
+        }
     } else {
         // ================================ dQ reducer ================================
-        // dQ_i (fp32, 128 x D) goes TMEM -> registers -> a staging buffer in 128-byte-swizzled rows of 32 floats, and from there to the
-        // fp32 accumulator with TMA reduce-add.  An SM's reduce engine moves about 19 bytes per clock, so it has to run all the time:
-        // with d = 64 two staging buffers alternate (the second one is the V tile, dead once V sits in tensor memory).
+        // dQ_i (fp32, 128 x D) goes TMEM -> registers -> one of two staging buffers in 128-byte-swizzled rows of 32 floats, and from there to
+        // the fp32 accumulator with TMA reduce-add.  An SM's reduce engine moves about 19 bytes per clock, so a buffer is only waited for
+        // when it comes round again.
         setmaxnreg_dec_48();
         const int r = ((warp & 3) << 5) | lane;
         const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
-        constexpr int kStgBufs = D == 64 ? 2 : 1;
-        for (int i = 0; i < n_q; ++i) {
-            mbar_wait(bar(kBarDqFull), i & 1, abort_flag, p.status, 350);
-            tc_fence_after();
-            const bool own = q_lo + i * kTile + r < n;              // rows behind the document get zeros, whatever K holds
+        int c = 0;
+        for (int k = 0; take(k); ++k) {
+            const int n_q = items[k & 1].q_tiles();
+            const int32_t n_own = items[k & 1].n - items[k & 1].q_lo, row0 = items[k & 1].node0 + items[k & 1].q_lo, col0 = items[k & 1].head * D;
+            give_back(k);
+            for (int i = 0; i < n_q; ++i, ++c) {
+                mbar_wait(bar(kBarDqFull), c & 1, abort_flag, p.status, 350);
+                tc_fence_after();
+                const bool own = i * kTile + r < n_own;             // rows behind the document get zeros, whatever K holds
 #pragma unroll
-            for (int c = 0; c < D / 32; ++c) {
-                uint8_t* stg = smem + (kStgBufs == 2 && c == 1 ? L::kV : L::kStg);
-                uint32_t o[32];
-                tmem_ld32(tmem + kColDq + c * 32 + lane_off, o);
-                tmem_wait_ld();
-                if (c == D / 32 - 1) { tc_fence_before(); __syncwarp(); if (lane == 0) mbar_arrive(bar(kBarDqFree)); }
-                if (warp == 20 && elect_one()) {        // the reduce that last used this buffer has read it
-                    if (kStgBufs == 2) bulk_wait_group_read1(); else bulk_wait_group_read0();
-                }
-                named_barrier_sync(kNbDqStagingFree, 128);
-                uint8_t* row = stg + r * 128;
+                for (int e = 0; e < D / 32; ++e) {
+                    uint8_t* stg = smem + L::kStg + ((c * (D / 32) + e) & 1) * 16384;
+                    uint32_t o[32];
+                    tmem_ld32(tmem + kColDq + e * 32 + lane_off, o);
+                    tmem_wait_ld();
+                    if (e == D / 32 - 1) { tc_fence_before(); __syncwarp(); if (lane == 0) mbar_arrive(bar(kBarDqFree)); }
+                    if (warp == 20 && elect_one()) bulk_wait_group_read1();        // the reduce that last used this buffer has read it
+                    named_barrier_sync(kNbDqStagingFree, 128);
+                    uint8_t* row = stg + r * 128;
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    *(uint4*)(row + ((k ^ (r & 7)) << 4)) = own ? make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]) : make_uint4(0u, 0u, 0u, 0u);
-                fence_proxy_async_smem();
-                named_barrier_sync(kNbDqStaged, 128);
-                if (warp == 20) {
-                    if (elect_one()) {
-                        tma_reduce_add_2d(&tmap_dq, smem_u32(stg), h * D + c * 32, node0 + q_lo + i * kTile);
-                        bulk_commit_group();
+                    for (int q = 0; q < 8; ++q)
+                        *(uint4*)(row + ((q ^ (r & 7)) << 4)) = own ? make_uint4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]) : make_uint4(0u, 0u, 0u, 0u);
+                    fence_proxy_async_smem();
+                    named_barrier_sync(kNbDqStaged, 128);
+                    if (warp == 20) {
+                        if (elect_one()) {
+                            tma_reduce_add_2d(&tmap_dq, smem_u32(stg), col0 + e * 32, row0 + i * kTile);
+                            bulk_commit_group();
+                        }
+                        __syncwarp();
                     }
-                    __syncwarp();
                 }
             }
         }
@@ -578,7 +689,7 @@ struct PrepareParams {
     int4* list;                // packed batch: work list of the main kernel, made by the last blocks
     const int32_t* cu_seqlens;
     size_t n_acc;              // float4s of them
-    int32_t n_total, n_graphs, n_heads;
+    int32_t n_total, n_graphs, n_heads, causal;
     uint32_t row_blocks;       // thread blocks that work on rows
     float sqrt_d;
 };
@@ -597,7 +708,7 @@ __global__ void __launch_bounds__(kPrepareThreads) position_prepare_kernel(const
     grid_release();
     if (blockIdx.x >= p.row_blocks) {
         const int32_t w = (int32_t)((blockIdx.x - p.row_blocks) * (kPrepareThreads / 32) + (threadIdx.x >> 5));
-        if (w < p.n_graphs) write_work_list<kTile>(p.list, p.n_total / kTile + p.n_graphs, p.cu_seqlens, p.n_graphs, w);
+        if (w < p.n_graphs) write_list<kTile>(p.list, p.n_total / kTile + p.n_graphs, p.cu_seqlens, p.n_graphs, w, p.causal);
         return;
     }
     const size_t n_rows = (size_t)p.n_total * p.n_heads, row0 = (size_t)blockIdx.x * kPrepareRows;
@@ -715,10 +826,8 @@ gt_status launch(const CUtensorMap (&maps)[6], PositionBwdParams p, const gt_bat
     static std::atomic<uint64_t> granted{0};
     const gt_status st = grant_smem(kern, granted, Smem<D>::kDynamic);
     if (st != GT_OK) return st;
-    const dim3 grid = p.list ? dim3((unsigned)(list_entries(batch, kTile) * p.n_heads))
-                             : dim3((unsigned)p.n_heads, (unsigned)((batch->max_seqlen + kTile - 1) / kTile), (unsigned)batch->n_graphs);
-    // With several waves of blocks the early start of the next kernel slows the dispatch of this one's.
-    p.early_release = (int64_t)grid.x * grid.y * grid.z <= sm_count();
+    const dim3 grid((unsigned)std::min(p.n_items, sm_count()));
+    p.early_release = p.n_items <= sm_count();
     return launch_overlapped(kern, grid, kThreads, Smem<D>::kDynamic, s, maps[0], maps[1], maps[2], maps[3], maps[4], maps[5], p);
 }
 
@@ -776,7 +885,15 @@ extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const vo
         p.dv_acc = p.dk_acc + (size_t)T * n_kv_heads * head_dim;
     }
     p.status = (uint32_t*)workspace;
-    if (batch->n_graphs > 1 && list_saves(batch, kTile, n_heads, 0)) p.list = (const int4*)(ws + w.list_off);
+    p.next_item = (uint32_t*)workspace + kNextBackward;
+    p.n_graphs = batch->n_graphs;
+    int64_t n_items = (int64_t)((batch->max_seqlen + kTile - 1) / kTile) * batch->n_graphs * n_heads;
+    if (batch->n_graphs > 1 && list_saves(batch, kTile, n_heads, 0)) {
+        p.list = (const int4*)(ws + w.list_off);
+        n_items = (int64_t)list_entries(batch, kTile) * n_heads;
+    }
+    if (n_items > 0x7fff0000) return GT_ERR_UNSUPPORTED;
+    p.n_items = (int32_t)n_items;
     p.n_total = T;
     p.n_heads = n_heads;
     p.group = n_heads / n_kv_heads;
@@ -800,6 +917,7 @@ extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const vo
     pre.n_total = T;
     pre.n_graphs = batch->n_graphs;
     pre.n_heads = n_heads;
+    pre.causal = p.causal;
     pre.row_blocks = (uint32_t)(((size_t)T * n_heads + kPrepareRows - 1) / kPrepareRows);
     pre.sqrt_d = sqrtf((float)head_dim);
     const uint32_t list_blocks = p.list ? (uint32_t)((batch->n_graphs + kPrepareThreads / 32 - 1) / (kPrepareThreads / 32)) : 0;
