@@ -689,7 +689,7 @@ struct PrepareParams {
     int4* list;                // packed batch: work list of the main kernel, made by the last blocks
     const int32_t* cu_seqlens;
     size_t n_acc;              // float4s of them
-    int32_t n_total, n_graphs, n_heads, causal;
+    int32_t n_total, n_graphs, n_heads, by_work;
     uint32_t row_blocks;       // thread blocks that work on rows
     float sqrt_d;
 };
@@ -708,7 +708,7 @@ __global__ void __launch_bounds__(kPrepareThreads) position_prepare_kernel(const
     grid_release();
     if (blockIdx.x >= p.row_blocks) {
         const int32_t w = (int32_t)((blockIdx.x - p.row_blocks) * (kPrepareThreads / 32) + (threadIdx.x >> 5));
-        if (w < p.n_graphs) write_list<kTile>(p.list, p.n_total / kTile + p.n_graphs, p.cu_seqlens, p.n_graphs, w, p.causal);
+        if (w < p.n_graphs) write_list<kTile>(p.list, p.n_total / kTile + p.n_graphs, p.cu_seqlens, p.n_graphs, w, p.by_work);
         return;
     }
     const size_t n_rows = (size_t)p.n_total * p.n_heads, row0 = (size_t)blockIdx.x * kPrepareRows;
@@ -777,30 +777,34 @@ struct FinishParams {
     __nv_bfloat16* to[3];
     int64_t row[3];            // elements from a row to the next
     float mul[3];
-    uint32_t vecs[3];          // groups of eight channels in a row, 0: nothing to do
+    uint32_t vecs[3];          // groups of four channels in a row
     const int32_t* cu_seqlens;
     int32_t n_total, n_graphs;
 };
 
-// The fp32 sums, scaled and rounded once; eight channels a thread.
-__global__ void __launch_bounds__(256) position_finish_kernel(const FinishParams p)
+// The fp32 sums, scaled and rounded once; a tensor per blockIdx.y, four groups of four channels a thread.
+constexpr int kFinishThreads = 256, kFinishEach = 4;
+__global__ void __launch_bounds__(kFinishThreads) position_finish_kernel(const __grid_constant__ FinishParams p)
 {
     grid_wait();
     grid_release();
-    const int32_t end = p.cu_seqlens ? p.cu_seqlens[p.n_graphs] : p.n_total;
-    const uint32_t all = p.vecs[0] + p.vecs[1] + p.vecs[2];
-    const uint64_t idx = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    const uint64_t t = idx / all;
-    if (t >= (uint64_t)end) return;
-    uint32_t c = (uint32_t)(idx - t * all);
-    int of = 0;
-    if (c >= p.vecs[0]) { c -= p.vecs[0]; of = 1; }
-    if (of == 1 && c >= p.vecs[1]) { c -= p.vecs[1]; of = 2; }
-    const float4* src = p.acc[of] + 2 * (t * p.vecs[of] + c);
-    const float4 a = __ldcs(src), b = __ldcs(src + 1);
+    const int of = blockIdx.y;
+    const uint32_t vecs = p.vecs[of];
+    const uint64_t all = (uint64_t)p.n_total * vecs, end = p.cu_seqlens ? (uint64_t)p.cu_seqlens[p.n_graphs] * vecs : all;
+    const uint64_t at = (uint64_t)blockIdx.x * (kFinishThreads * kFinishEach) + threadIdx.x;
+    const float4* acc = p.acc[of];
     const float m = p.mul[of];
-    *(uint4*)(p.to[of] + (int64_t)t * p.row[of] + 8 * (int64_t)c) =
-        make_uint4(pack_bf16x2(a.x * m, a.y * m), pack_bf16x2(a.z * m, a.w * m), pack_bf16x2(b.x * m, b.y * m), pack_bf16x2(b.z * m, b.w * m));
+    float4 v[kFinishEach];
+#pragma unroll
+    for (int i = 0; i < kFinishEach; ++i)
+        if (at + i * kFinishThreads < end) v[i] = __ldcs(acc + at + i * kFinishThreads);
+#pragma unroll
+    for (int i = 0; i < kFinishEach; ++i) {
+        const uint64_t idx = at + i * kFinishThreads;
+        if (idx >= end) continue;
+        const uint64_t t = all >> 32 ? idx / vecs : (uint32_t)idx / vecs;
+        *(uint2*)(p.to[of] + (int64_t)t * p.row[of] + 4 * (int64_t)(idx - t * vecs)) = make_uint2(pack_bf16x2(v[i].x * m, v[i].y * m), pack_bf16x2(v[i].z * m, v[i].w * m));
+    }
 }
 
 struct Workspace {
@@ -917,7 +921,7 @@ extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const vo
     pre.n_total = T;
     pre.n_graphs = batch->n_graphs;
     pre.n_heads = n_heads;
-    pre.causal = p.causal;
+    pre.by_work = list_by_work(batch, causal, (size_t)T * n_heads * head_dim * 8);
     pre.row_blocks = (uint32_t)(((size_t)T * n_heads + kPrepareRows - 1) / kPrepareRows);
     pre.sqrt_d = sqrtf((float)head_dim);
     const uint32_t list_blocks = p.list ? (uint32_t)((batch->n_graphs + kPrepareThreads / 32 - 1) / (kPrepareThreads / 32)) : 0;
@@ -937,12 +941,12 @@ extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const vo
         f.to[i] = (__nv_bfloat16*)to[i];
         f.row[i] = row[3 + i];
         f.mul[i] = i < 2 ? p.scale : 1.0f;
-        f.vecs[i] = acc[i] ? (uint32_t)((i == 0 ? n_heads : n_kv_heads) * head_dim / 8) : 0u;
+        f.vecs[i] = (uint32_t)((i == 0 ? n_heads : n_kv_heads) * head_dim / 4);
     }
     f.cu_seqlens = batch->cu_seqlens;
     f.n_total = T;
     f.n_graphs = batch->n_graphs;
-    const uint64_t threads = (uint64_t)T * (f.vecs[0] + f.vecs[1] + f.vecs[2]);
-    if ((threads + 255) / 256 > 0x7fffffffull) return GT_ERR_UNSUPPORTED;
-    return launch_overlapped(position_finish_kernel, dim3((unsigned)((threads + 255) / 256)), 256, 0, s, f);
+    const uint64_t blocks = ((uint64_t)T * f.vecs[0] + kFinishThreads * kFinishEach - 1) / (kFinishThreads * kFinishEach);
+    if (blocks > 0x7fffffffull) return GT_ERR_UNSUPPORTED;
+    return launch_overlapped(position_finish_kernel, dim3((unsigned)blocks, w.kv_bytes > 0 ? 3u : 1u), kFinishThreads, 0, s, f);
 }

@@ -678,12 +678,12 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 
 // Work list of a packed batch, a warp per document.
 constexpr int kListThreads = 128;
-__global__ void __launch_bounds__(kListThreads) position_list_kernel(int4* list, int32_t entries, const int32_t* cu_seqlens, int32_t n_graphs, int32_t causal)
+__global__ void __launch_bounds__(kListThreads) position_list_kernel(int4* list, int32_t entries, const int32_t* cu_seqlens, int32_t n_graphs, bool by_work)
 {
     grid_wait();
     grid_release();
     const int32_t w = (int32_t)((blockIdx.x * blockDim.x + threadIdx.x) >> 5);
-    if (w < n_graphs) write_list<2 * kTile>(list, entries, cu_seqlens, n_graphs, w, causal);
+    if (w < n_graphs) write_list<2 * kTile>(list, entries, cu_seqlens, n_graphs, w, by_work);
 }
 constexpr size_t kListMinSaved = 256;        // empty items that the list has to save: it costs a launch
 
@@ -758,7 +758,7 @@ extern "C" gt_status gt_position_attn_fwd(const void* q, const void* k, const vo
         n_items = (int64_t)list_entries(batch, rows) * n_heads;
         const unsigned blocks = (unsigned)((batch->n_graphs + kListThreads / 32 - 1) / (kListThreads / 32));
         if ((st = launch_overlapped(position_list_kernel, dim3(blocks), kListThreads, 0, s, list, (int32_t)list_entries(batch, rows), batch->cu_seqlens,
-                                    batch->n_graphs, p.causal)) != GT_OK)
+                                    batch->n_graphs, list_by_work(batch, causal, (size_t)batch->n_total * n_kv_heads * head_dim * 4))) != GT_OK)
             return st;
     }
     if (n_items > 0x7fff0000) return GT_ERR_UNSUPPORTED;
