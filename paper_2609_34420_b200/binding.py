@@ -531,17 +531,21 @@ def gt_feature_code_dweights(dtable, vectors, dweights) -> None:
 
 
 def _rows(t: Optional[torch.Tensor]):
-    """Address and row stride of a [T, heads, d] tensor whose rows are contiguous, but may lie apart (parts of a projection)."""
+    """Address and row stride (0: packed) of a [T, heads, d] tensor whose rows are contiguous, but may lie apart (parts of a projection)."""
     if t is None:
         return None, 0
-    if not t.is_cuda or t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
-        raise ValueError("expected a CUDA tensor [T, heads, d] with contiguous rows")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0
+    if not t.is_cuda:
+        raise ValueError("expected a CUDA tensor")
+    if t.is_contiguous():
+        return t.data_ptr(), 0
+    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise ValueError("expected a tensor [T, heads, d] with contiguous rows")
+    return t.data_ptr(), t.stride(0)
 
 
 def _same_dtype(dtype, *tensors) -> None:
     for t in tensors:
-        if t is not None and t.dtype != dtype:
+        if t is not None and t.dtype is not dtype:
             raise ValueError(f"expected tensors of type {dtype}")
 
 
@@ -550,10 +554,10 @@ def gt_position_attn_fwd_workspace(batch: Batch, n_heads: int, n_kv_heads: int, 
     return int(lib().gt_position_attn_fwd_workspace(b, n_heads, n_kv_heads, head_dim))
 
 
-def _position_strides(q, k, v, dq=None, dk=None, dv=None):
-    """C struct of the row strides, and the addresses."""
-    got = [_rows(t) for t in (q, k, v, dq, dk, dv)]
-    return _GtRowStrides(*[s for _, s in got]), [p for p, _ in got]
+def _position_strides(*tensors):
+    """Reference to the C struct of the row strides of q, k, v(, dq, dk, dv), None where all are packed, and the addresses."""
+    pointers, strides = zip(*[_rows(t) for t in tensors])
+    return (ctypes.byref(_GtRowStrides(*strides)) if any(strides) else None), pointers
 
 
 def gt_position_attn_fwd(q, k, v, slopes: Optional[torch.Tensor], prefix: Optional[torch.Tensor], batch: Batch,
@@ -568,8 +572,8 @@ def gt_position_attn_fwd(q, k, v, slopes: Optional[torch.Tensor], prefix: Option
     _same_dtype(torch.int32, prefix)
     if workspace is None:
         workspace = _workspace(gt_position_attn_fwd_workspace(batch, H, G, d), q.device)
-    strides, (pq, pk, pv, _, _, _) = _position_strides(q, k, v)
-    st = lib().gt_position_attn_fwd(pq, pk, pv, _ptr(slopes), _ptr(prefix), batch._c_pair()[1], H, G, d, ctypes.byref(strides),
+    strides, (pq, pk, pv) = _position_strides(q, k, v)
+    st = lib().gt_position_attn_fwd(pq, pk, pv, _ptr(slopes), _ptr(prefix), batch._c_pair()[1], H, G, d, strides,
                                     int(causal), float(cap), _ptr(out), _ptr(lse), _ptr(out_f32), _ptr(workspace), workspace.numel(), _stream())
     _raise(st, "gt_position_attn_fwd")
     return workspace
@@ -593,7 +597,7 @@ def gt_position_attn_bwd(q, k, v, out, dout, lse, slopes: Optional[torch.Tensor]
         workspace = _workspace(gt_position_attn_bwd_workspace(batch, H, G, d), q.device)
     strides, (pq, pk, pv, pdq, pdk, pdv) = _position_strides(q, k, v, dq, dk, dv)
     st = lib().gt_position_attn_bwd(pq, pk, pv, _ptr(out), _ptr(out_f32), _ptr(dout), _ptr(lse), _ptr(slopes), _ptr(prefix), batch._c_pair()[1],
-                                    H, G, d, ctypes.byref(strides), int(causal), float(cap), pdq, pdk, pdv,
+                                    H, G, d, strides, int(causal), float(cap), pdq, pdk, pdv,
                                     _ptr(workspace), workspace.numel(), _stream())
     _raise(st, "gt_position_attn_bwd")
     return workspace
