@@ -43,6 +43,31 @@ __device__ __forceinline__ uint64_t tanh_ratio(uint64_t u)
     r = sm100::fma_f32x2(r, u, both(kTanh1));
     return sm100::fma_f32x2(r, u, both(kTanh0));
 }
+constexpr float kEx2_0 = 9.999992614e-01f, kEx2_1 = 6.931218147e-01f, kEx2_2 = 2.402474483e-01f, kEx2_3 = 5.591786032e-02f, kEx2_4 = 9.570101911e-03f;
+// 2^x of two arguments without the special-function unit: with n the whole number next to x, 2^(x - n) is a polynomial of degree 4 (by the
+// exchange method; off by at most 2.6e-6 relative, a thousandth of what a probability loses to bf16) and n goes into the
+// exponent by an integer addition.  x is held within [-126, 127]: below, the result is as good as 0; above, and for a NaN, it is far beyond
+// what a sum of a tile may be.
+__device__ __forceinline__ void ex2_pair(uint64_t x, float& lo, float& hi)
+{
+    float a, b;
+    sm100::unpack_f32x2(x, a, b);
+    asm("max.NaN.f32 %0, %0, 0fC2FC0000;\n\tmin.NaN.f32 %0, %0, 0f42FE0000;" : "+f"(a));
+    asm("max.NaN.f32 %0, %0, 0fC2FC0000;\n\tmin.NaN.f32 %0, %0, 0f42FE0000;" : "+f"(b));
+    x = sm100::pack_f32x2(a, b);
+    const uint64_t t = sm100::add_f32x2(x, both(0x1.8p23f));
+    const uint64_t f = sm100::fma_f32x2(sm100::add_f32x2(t, both(-0x1.8p23f)), both(-1.f), x);
+    uint64_t r = sm100::fma_f32x2(both(kEx2_4), f, both(kEx2_3));
+    r = sm100::fma_f32x2(r, f, both(kEx2_2));
+    r = sm100::fma_f32x2(r, f, both(kEx2_1));
+    r = sm100::fma_f32x2(r, f, both(kEx2_0));
+    float t0, t1, r0, r1;
+    sm100::unpack_f32x2(t, t0, t1);
+    sm100::unpack_f32x2(r, r0, r1);
+    lo = __uint_as_float(__float_as_uint(r0) + (__float_as_uint(t0) << 23));
+    hi = __uint_as_float(__float_as_uint(r1) + (__float_as_uint(t1) << 23));
+}
+
 // tanh(y) of any y: the polynomial within its reach, beyond it 1 - 2 / (1 + e^2y), which is off by 3e-7.
 __device__ __forceinline__ float tanh_any(float y)
 {

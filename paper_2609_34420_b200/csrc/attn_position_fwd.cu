@@ -26,6 +26,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "attn_position.cuh"
 
@@ -43,6 +44,10 @@ constexpr float kSumThreshold = 0x1p24f;       // tile row sum above which the r
 // Scores of a capped row lie within cap log2(e) of 0 at the diagonal, so that against a reference of half of that the largest P is between 2^-108 and
 // 2^37: sums, products with v of up to 2^60 and their sums stay within fp32, and nothing that counts is lost below.
 constexpr float kBoundedCap = 50.0f;
+// Every eighth pair of exponentials is a polynomial's (ex2_pair), which takes load off the special-function unit (77 % busy without) and adds
+// to the issue slots: 16 384 tokens, 8 heads of 64, all pairs 768 -> 710 us (every sixth 746, every fourth 749, every third 790), causal 372 ->
+// 344, causal with the fp32 output 428 -> 409; with the penalty on distance 411 -> 407, and with both 457 -> 475, so not there.
+constexpr int kEx2Every = 8;
 constexpr float kPeekReach = 24.0f;            // log2 units within which a row's first scores leave the starting reference as it is
 
 struct PositionFwdParams {
@@ -56,6 +61,7 @@ struct PositionFwdParams {
     uint32_t* next_item;       // counts the items that have been taken beyond the grid's first ones; 0 before and after the kernel
     const int4* list;          // packed batch: work list; item = entry * heads + head (nullptr: heads, then documents, then blocks)
     int32_t n_items;
+    int32_t halves_from;       // without a list: rows of items (all heads of a block) from this one on are halved
     int32_t n_graphs;
     int32_t n_total;
     int32_t n_heads;
@@ -101,22 +107,19 @@ struct Smem {
 };
 
 struct alignas(16) Item {
-    int32_t node0, n, head, q_block;       // n = 0: there are no more
-    int32_t prefix, pad[3];
+    int32_t node0, n, head, prefix;        // n = 0: there are no more
+    int32_t first, tiles, pad[2];          // the item's query tiles
 };
 
 // What follows from an item: its query tiles and the key tiles that they see.
 struct Span {
     int32_t q0, tiles, diagonal, n_kv, skip;
-    // kTiles query tiles per block, counted from the document's end
-    template <int kTiles>
     __device__ __forceinline__ void set(const Item& item, bool causal)
     {
-        const int32_t n_tiles = (item.n + kTile - 1) / kTile, odd = kTiles == 2 ? n_tiles & 1 : 0, first = max(0, item.q_block * kTiles - odd);
-        tiles = kTiles == 2 && odd && item.q_block == 0 ? 1 : kTiles;
-        q0 = first * kTile;
-        diagonal = first + tiles - 1;
-        n_kv = causal ? max(diagonal + 1, (min(item.n, item.prefix) + kTile - 1) / kTile) : n_tiles;
+        tiles = item.tiles;
+        q0 = item.first * kTile;
+        diagonal = item.first + tiles - 1;
+        n_kv = causal ? max(diagonal + 1, (min(item.n, item.prefix) + kTile - 1) / kTile) : (item.n + kTile - 1) / kTile;
         // key tiles that the first query tile does not see: the item's first one, or none
         skip = tiles == 2 && causal && item.prefix <= diagonal * kTile ? 1 : 0;
     }
@@ -218,7 +221,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         index = (int32_t)(gridDim.x + __shfl_sync(0xffffffffu, taken, 0));
                     }
                     if (index >= p.n_items) break;
-                    int32_t g, block;
+                    int32_t g, block, part = -1;              // part: of a block that is halved
                     if (p.list) {
                         const int4 entry = p.list[index / p.n_heads];
                         g = entry.x;
@@ -226,7 +229,11 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         item.node0 = entry.z;
                         item.n = entry.x < 0 ? 0 : entry.w;
                     } else {
-                        const int32_t row = index / p.n_heads;
+                        int32_t row = index / p.n_heads;
+                        if (kTiles == 2 && row >= p.halves_from) {
+                            part = (row - p.halves_from) & 1;
+                            row = p.halves_from + (row - p.halves_from) / 2;
+                        }
                         block = row / p.n_graphs;
                         g = row % p.n_graphs;
                         item.node0 = p.cu_seqlens ? p.cu_seqlens[g] : 0;
@@ -234,8 +241,16 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     }
                     item.head = index % p.n_heads;
                     index = -1;
-                    const int32_t n_blocks = (item.n + kTiles * kTile - 1) / (kTiles * kTile);
-                    item.q_block = p.causal ? n_blocks - 1 - block : block;
+                    // blocks of kTiles query tiles, counted from the document's end
+                    const int32_t n_tiles = (item.n + kTile - 1) / kTile, n_blocks = (n_tiles + kTiles - 1) / kTiles, odd = n_blocks * kTiles - n_tiles;
+                    const int32_t q_block = p.causal ? n_blocks - 1 - block : block;
+                    item.first = max(0, q_block * kTiles - odd);
+                    item.tiles = kTiles == 2 && odd && q_block == 0 ? 1 : kTiles;
+                    if (part >= 0) {
+                        if (part == 1 && item.tiles == 1) block = n_blocks;       // (there is no other half)
+                        item.first += part;
+                        item.tiles = 1;
+                    }
                     if (block >= n_blocks) item.n = 0;
                     else item.prefix = p.prefix ? p.prefix[g] : 0;
                 }
@@ -252,7 +267,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             Span span;
             int c = 0;                                       // key tiles so far
             for (int k = 0; take(k, item); ++k) {
-                span.set<kTiles>(item, p.causal);
+                span.set(item, p.causal);
                 const int kv_head = item.head / p.group;
                 if (k >= 2) mbar_wait(bar(kBarQEmpty + (k & 1)), ((k >> 1) & 1) ^ 1, abort_flag, p.status, 210);
                 if (lane == 0) {
@@ -289,7 +304,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             int c = 0, step = 0;                             // key tiles, and score tiles, so far
             int own[2][2] = {{-4, -4}, {-4, -4}}, done[2] = {0, 0};      // each query tile's last two steps, and how many there were
             for (int k = 0; take(k, item); ++k) {
-                span.set<kTiles>(item, p.causal);
+                span.set(item, p.causal);
                 mbar_wait(bar(kBarQFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 220);
                 for (int s = 0; s < span.n_kv; ++s, ++c) {
                     const int ks = c % kStages;
@@ -331,7 +346,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             Span span;
             int c = 0, step = 0, own[2] = {0, 0};            // key tiles, score tiles and each query tile's so far
             for (int k = 0; take(k, item); ++k) {
-                span.set<kTiles>(item, p.causal);
+                span.set(item, p.causal);
                 // the document's last V tile, if rows of another one follow in it
                 const int32_t ragged_tile = item.n % kTile != 0 && item.node0 + item.n < p.n_total ? item.n / kTile : -1;
                 for (int s = 0; s < span.n_kv; ++s, ++c) {
@@ -386,7 +401,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         mbar_wait(bar(kBarItemFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 202);
         if (items[k & 1].n == 0 || *abort_flag != 0u) break;
         Span span;
-        span.set<kTiles>(items[k & 1], p.causal);
+        span.set(items[k & 1], p.causal);
         const int32_t first = t == 0 ? span.skip : 0, diagonal = span.diagonal, step_by = span.tiles;
         int32_t key_tile = span.key_tile(first), left = t < span.tiles ? span.n_kv - first : 0;       // left: steps
         int step = step0 + (span.tiles == 2 ? 2 * first + t - span.skip : 0);
@@ -576,7 +591,14 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                                 if (c * kCW + e + i >= valid) x[i] = -INFINITY;
                                 if (c * kCW + e + i + 1 >= valid) x[i + 1] = -INFINITY;
                             }
-                            const float lo = ex2_approx(x[i]), hi = ex2_approx(x[i + 1]);
+                            float lo, hi;
+                            // (never behind the classical way: a NaN would not come through)
+                            if (!decltype(rag)::value && !(kSlope && kExact) && ((c * kCW + e + i) / 2) % kEx2Every == kEx2Every - 1) {
+                                ex2_pair(pack_f32x2(x[i], x[i + 1]), lo, hi);
+                            } else {
+                                lo = ex2_approx(x[i]);
+                                hi = ex2_approx(x[i + 1]);
+                            }
                             sum2 = add_f32x2(sum2, pack_f32x2(lo, hi));
                             const uint32_t w = pk[(c * kCW + e + i) >> 1] = pack_bf16x2(lo, hi);
                             if constexpr (kExact) rounded2 = add_f32x2(rounded2, pack_u32x2(w << 16, w & 0xffff0000u));
@@ -591,7 +613,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     tmem_wait_ld(); exp_chunk(3, sb, rag, general);
                 };
                 if (mixed || (kCap && (exact || wide))) exp_pass(Tag<true>{}, Tag<kCap || kSlope>{});
-                else if (ragged) exp_pass(Tag<true>{}, Tag<false>{});
+                else if (ragged || exact) exp_pass(Tag<true>{}, Tag<false>{});
                 else exp_pass(Tag<false>{}, Tag<false>{});
                 loaded = false;
                 {
@@ -687,6 +709,26 @@ __global__ void __launch_bounds__(kListThreads) position_list_kernel(int4* list,
 }
 constexpr size_t kListMinSaved = 256;        // empty items that the list has to save: it costs a launch
 
+// Blocks of one query tile, a CTA for each, or of two?  A key tile takes about 1.0 us with one query tile and 1.4 us with two, so that two are
+// faster where the grid fills the device; the longest block (causal: the last one) has to be through all the same.
+inline bool one_tile_blocks(const gt_batch* b, int32_t n_heads, bool causal)
+{
+#ifdef GT_FORCE_ROWS
+    return GT_FORCE_ROWS == 128;
+#endif
+    const double tiles = (b->max_seqlen + kTile - 1) / kTile, pairs = (b->max_seqlen + 2 * kTile - 1) / (2 * kTile);
+    const double m = (double)b->n_graphs * n_heads, sms = sm_count();
+    const double one = causal ? std::max(tiles, m * tiles * (tiles + 1) / 2 / sms) : std::ceil(m * tiles / sms) * tiles;
+    const double two = causal ? std::max(tiles, m * pairs * (pairs + 1) / sms) : std::ceil(m * pairs / sms) * tiles;
+    return 1.0 * one < 1.4 * two;
+}
+// Blocks of one long document, all of one length, that are halved so that the grid's last wave is one of halves.
+inline int32_t halved_blocks(int32_t blocks, int32_t n_heads)
+{
+    const int64_t all = (int64_t)blocks * n_heads, whole = all / sm_count() * sm_count() / n_heads;       // blocks in full waves
+    return 2 * (all - whole * n_heads) <= sm_count() ? (int32_t)(blocks - whole) : 0;
+}
+
 template <int D, int kCapForm, bool kSlope, bool kExact>
 gt_status launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, PositionFwdParams p, const gt_batch* batch, int32_t rows,
                  cudaStream_t s)
@@ -748,10 +790,16 @@ extern "C" gt_status gt_position_attn_fwd(const void* q, const void* k, const vo
     p.to_tanh = cap > 0.f ? 1.0f / (sqrtf((float)head_dim) * cap) : 0.f;
     p.cap2 = cap * kLog2e;
     cudaStream_t s = (cudaStream_t)stream;
-    // Blocks of one query tile where those of two would leave half of the SMs idle or more.
-    const int32_t rows = (int64_t)((batch->max_seqlen + kTile - 1) / kTile) * batch->n_graphs * n_heads <= sm_count() ? kTile : 2 * kTile;
     p.n_graphs = batch->n_graphs;
-    int64_t n_items = (int64_t)((batch->max_seqlen + rows - 1) / rows) * batch->n_graphs * n_heads;
+    const int32_t rows = one_tile_blocks(batch, n_heads, causal != 0) ? kTile : 2 * kTile;
+    const int32_t blocks = (batch->max_seqlen + rows - 1) / rows;
+    int64_t n_items = (int64_t)blocks * batch->n_graphs * n_heads;
+    p.halves_from = blocks * batch->n_graphs;
+    if (rows == 2 * kTile && batch->n_graphs == 1 && !causal) {
+        const int32_t halved = halved_blocks(blocks, n_heads);
+        p.halves_from -= halved;
+        n_items += (int64_t)halved * n_heads;
+    }
     if (batch->n_graphs > 1 && rows == 2 * kTile && list_saves(batch, rows, n_heads, kListMinSaved)) {
         int4* list = (int4*)((uint8_t*)workspace + kHeaderBytes);
         p.list = list;
