@@ -436,10 +436,10 @@ gt_status gt_feature_code_dweights(const float* dtable, const uint32_t* vectors,
  *     dv_j = sum P_ij dout_i,   dS_ij = P_ij (dout_i . v_j - Delta_i) (1 - tanh^2(x_ij / cap)),
  *     dq_i = sum_j dS_ij k_j / sqrt(d),   dk_j = sum dS_ij q_i / sqrt(d),
  * dk and dv summed over the query heads that share a key head.  dq, dk, dv (bf16) are overwritten; they must not overlap any
- * input.  dq, and with shared key heads dk and dv, are accumulated with floating-point atomics in fp32: their low-order bits may
- * differ from run to run.
+ * input.  dq, and where several thread blocks share a key's queries dk and dv (shared key heads, small batches), are accumulated with
+ * floating-point atomics in fp32: their low-order bits may differ from run to run.
  * Workspace as for every call (header zero at first).  Forward: 256 bytes and 16 per document and per 256 rows; backward:
- * (4 d + 32) bytes per row and query head, 8 d per row and key head where heads share keys, and 16 per document and 128 rows.
+ * (4 d + 32) bytes per row and query head, 8 d per row and key head, and 16 per document and 128 rows.
  * A query with bad arguments returns 0.
  * ------------------------------------------------------------------------------------- */
 typedef struct gt_row_strides {

@@ -26,6 +26,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "attn_position.cuh"
 
@@ -51,12 +52,13 @@ struct PositionBwdParams {
     __nv_bfloat16* dk;
     __nv_bfloat16* dv;
     int64_t dk_row, dv_row;  // elements from a row to the next
-    float* dk_acc;           // [T,G,D] fp32 (workspace, zeroed) where heads share keys, else nullptr
+    float* dk_acc;           // [T,G,D] fp32 (workspace, zeroed) where several items add to a key's row, else nullptr
     float* dv_acc;
     uint32_t* status;
     uint32_t* next_item;     // counts the items that have been taken beyond the grid's first ones; 0 before and after the kernel
     const int4* list;        // packed batch: work list; item = entry * heads + head (nullptr: heads, then documents, then tiles)
     int32_t n_items;
+    int32_t parts;           // without a list: items that share the queries of a key tile (then dk_acc and dv_acc are used)
     int32_t n_graphs;
     int32_t n_total;
     int32_t n_heads;
@@ -116,10 +118,11 @@ struct Smem {
 
 struct alignas(16) Item {
     int32_t node0, n, head, kv0;           // n = 0: there are no more
-    int32_t prefix, q_lo, pad[2];          // q_lo: first query that sees a key of the tile, in whole tiles
-    __device__ __forceinline__ int32_t q_tiles() const { return (n - q_lo + kTile - 1) / kTile; }
-    // rows of the last query tile that are the document's, if rows of another one follow in it, else 0
-    __device__ __forceinline__ int32_t ragged(int32_t n_total) const { return node0 + n < n_total ? n % kTile : 0; }
+    int32_t prefix, q_lo, q_hi, pad;       // queries [q_lo, q_hi): those that see a key of the tile, in whole tiles, or a part of them
+    __device__ __forceinline__ int32_t q_tiles() const { return (q_hi - q_lo + kTile - 1) / kTile; }
+    // rows of the last query tile, and of the key tile, that are the document's, if rows of another one follow in it, else 0
+    __device__ __forceinline__ int32_t ragged(int32_t n_total) const { return q_hi == n && node0 + n < n_total ? n % kTile : 0; }
+    __device__ __forceinline__ int32_t ragged_keys(int32_t n_total) const { return kv0 + kTile > n && node0 + n < n_total ? n % kTile : 0; }
 };
 
 // register budget: the CTA is launched with 768 x 80 registers; after the re-split it holds
@@ -223,7 +226,7 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         index = (int32_t)(gridDim.x + __shfl_sync(0xffffffffu, taken, 0));
                     }
                     if (index >= p.n_items) break;
-                    int32_t g, tile;
+                    int32_t g, tile, part = 0;
                     if (p.list) {
                         const int4 entry = p.list[index / p.n_heads];
                         g = entry.x;
@@ -231,7 +234,9 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         item.node0 = entry.z;
                         item.n = entry.x < 0 ? 0 : entry.w;
                     } else {
-                        const int32_t row = index / p.n_heads;
+                        int32_t row = index / p.n_heads;
+                        part = row % p.parts;
+                        row /= p.parts;
                         tile = row / p.n_graphs;
                         g = row % p.n_graphs;
                         item.node0 = p.cu_seqlens ? p.cu_seqlens[g] : 0;
@@ -245,6 +250,13 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     } else {
                         item.prefix = p.prefix ? p.prefix[g] : 0;
                         item.q_lo = p.causal && item.kv0 >= item.prefix ? item.kv0 : 0;
+                        item.q_hi = item.n;
+                        if (p.parts > 1) {
+                            const int32_t each = (item.q_tiles() + p.parts - 1) / p.parts * kTile;
+                            item.q_lo += part * each;
+                            item.q_hi = min(item.n, item.q_lo + each);
+                            if (item.q_lo >= item.n) item.n = 0;
+                        }
                     }
                 }
                 if (k >= 2) mbar_wait(bar(kBarItemEmpty + (k & 1)), ((k >> 1) & 1) ^ 1, abort_flag, p.status, 301);
@@ -357,12 +369,12 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             int c = 0;
             for (int k = 0; take(k); ++k) {
                 const int n_q = items[k & 1].q_tiles();
-                const int q_rows = items[k & 1].ragged(p.n_total), k_rows = q_rows != 0 ? items[k & 1].n - items[k & 1].kv0 : kTile;
+                const int q_rows = items[k & 1].ragged(p.n_total), k_rows = items[k & 1].ragged_keys(p.n_total);
                 give_back(k);
                 uint8_t* const s_k = smem + L::kK + (k & 1) * L::kTileBytes;
                 const uint64_t desc_k = make_smem_desc(smem_u32(s_k), L::kRowBytes, 0);
                 mbar_wait(bar(kBarKFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 330);
-                if (k_rows < kTile) clear_rows(s_k, k_rows, L::kRowBytes);
+                if (k_rows != 0) clear_rows(s_k, k_rows, L::kRowBytes);
                 auto clear_tile = [&](int at) {                // tile number `at`, the item's last one, before any MMA reads it
                     mbar_wait(bar(kBarQdoFull + (at & 1)), (at >> 1) & 1, abort_flag, p.status, 331);
                     clear_rows(smem + L::kQ + (at & 1) * L::kStageBytes, q_rows, L::kRowBytes);
@@ -818,9 +830,27 @@ Workspace workspace_of(const gt_batch* b, int32_t n_heads, int32_t n_kv_heads, i
     w.list_off = kHeaderBytes;
     w.ext_off = w.list_off + list_bytes(b, kTile);
     w.acc_off = w.ext_off + align_up(rows * kExtCols * 2, 256);
-    w.kv_bytes = n_heads > n_kv_heads ? (size_t)b->n_total * n_kv_heads * head_dim * sizeof(float) : 0;
+    w.kv_bytes = (size_t)b->n_total * n_kv_heads * head_dim * sizeof(float);
     w.total = w.acc_off + align_up(rows * head_dim * sizeof(float) + 2 * w.kv_bytes, 256);
     return w;
+}
+
+// Items that share the queries of a key tile, where the longest one would hold up the rest: a query tile takes about 1.8 us, an item's fill
+// and drain 2, sums of dk and dv in memory 4 and 6 for every million of their elements (where heads share keys there are such sums
+// anyway).  One item -> this many, causal, 8 heads of 64 if not said otherwise: 4 096 tokens, 2 heads 59 -> 40 us, all pairs 61 -> 44;
+// 3 000 tokens, all pairs 107 -> 92; 2 048 tokens 38.7 -> 38.0; but 4 096 tokens 65 -> 79 and 8 192 tokens 200 -> 226, which stay with one.
+inline int32_t parts_of(const gt_batch* b, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, bool causal)
+{
+    const double tiles = (b->max_seqlen + kTile - 1) / kTile, m = (double)b->n_graphs * n_heads, sms = sm_count();
+    const double sums = n_heads > n_kv_heads ? 1.0 : 4.0 + 6e-6 * b->n_total * n_kv_heads * head_dim;
+    int32_t best = 1;
+    double least = 1e30;
+    for (int32_t parts = 1; parts <= 4 && parts <= tiles; parts *= 2) {
+        const double longest = std::ceil(tiles / parts), all = m * tiles * (causal ? (tiles + 1) / 2 : tiles) / sms, waves = std::ceil(m * tiles * parts / sms);
+        const double us = 1.8 * (causal ? std::max(longest, all) : std::max(all, waves * longest)) + 2.0 * waves + sums * (parts / 2);
+        if (us < 0.95 * least) { least = us; best = parts; }
+    }
+    return best;
 }
 
 template <int D, bool kCap, bool kSlope>
@@ -884,14 +914,16 @@ extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const vo
     p.dv = (__nv_bfloat16*)dv;
     p.dk_row = row[4];
     p.dv_row = row[5];
-    if (w.kv_bytes > 0) {
+    p.parts = batch->n_graphs > 1 && list_saves(batch, kTile, n_heads, 0) ? 1 : parts_of(batch, n_heads, n_kv_heads, head_dim, causal != 0);
+    const bool sums = n_heads > n_kv_heads || p.parts > 1;
+    if (sums) {
         p.dk_acc = dq_acc + (size_t)T * n_heads * head_dim;
         p.dv_acc = p.dk_acc + (size_t)T * n_kv_heads * head_dim;
     }
     p.status = (uint32_t*)workspace;
     p.next_item = (uint32_t*)workspace + kNextBackward;
     p.n_graphs = batch->n_graphs;
-    int64_t n_items = (int64_t)((batch->max_seqlen + kTile - 1) / kTile) * batch->n_graphs * n_heads;
+    int64_t n_items = (int64_t)((batch->max_seqlen + kTile - 1) / kTile) * batch->n_graphs * n_heads * p.parts;
     if (batch->n_graphs > 1 && list_saves(batch, kTile, n_heads, 0)) {
         p.list = (const int4*)(ws + w.list_off);
         n_items = (int64_t)list_entries(batch, kTile) * n_heads;
@@ -917,7 +949,7 @@ extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const vo
     pre.acc = (float4*)dq_acc;
     pre.list = const_cast<int4*>(p.list);
     pre.cu_seqlens = batch->cu_seqlens;
-    pre.n_acc = ((size_t)T * n_heads * head_dim * sizeof(float) + 2 * w.kv_bytes) / 16;
+    pre.n_acc = ((size_t)T * n_heads * head_dim * sizeof(float) + (sums ? 2 * w.kv_bytes : 0)) / 16;
     pre.n_total = T;
     pre.n_graphs = batch->n_graphs;
     pre.n_heads = n_heads;
@@ -948,5 +980,5 @@ extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const vo
     f.n_graphs = batch->n_graphs;
     const uint64_t blocks = ((uint64_t)T * f.vecs[0] + kFinishThreads * kFinishEach - 1) / (kFinishThreads * kFinishEach);
     if (blocks > 0x7fffffffull) return GT_ERR_UNSUPPORTED;
-    return launch_overlapped(position_finish_kernel, dim3((unsigned)blocks, w.kv_bytes > 0 ? 3u : 1u), kFinishThreads, 0, s, f);
+    return launch_overlapped(position_finish_kernel, dim3((unsigned)blocks, sums ? 3u : 1u), kFinishThreads, 0, s, f);
 }

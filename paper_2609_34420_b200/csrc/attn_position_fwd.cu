@@ -713,9 +713,6 @@ constexpr size_t kListMinSaved = 256;        // empty items that the list has to
 // faster where the grid fills the device; the longest block (causal: the last one) has to be through all the same.
 inline bool one_tile_blocks(const gt_batch* b, int32_t n_heads, bool causal)
 {
-#ifdef GT_FORCE_ROWS
-    return GT_FORCE_ROWS == 128;
-#endif
     const double tiles = (b->max_seqlen + kTile - 1) / kTile, pairs = (b->max_seqlen + 2 * kTile - 1) / (2 * kTile);
     const double m = (double)b->n_graphs * n_heads, sms = sm_count();
     const double one = causal ? std::max(tiles, m * tiles * (tiles + 1) / 2 / sms) : std::ceil(m * tiles / sms) * tiles;
