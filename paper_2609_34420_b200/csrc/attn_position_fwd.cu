@@ -464,15 +464,17 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             // Scores of eight consecutive columns in log2 units, plus `add`; general: any score, any distance.
             float top_u = 0.f;
             auto scores8 = [&](const uint32_t* sr, int col, float add, auto rag, auto general, float (&x)[8]) {
-                uint64_t base = both(add);
-                if constexpr (kSlope)
-                    if constexpr (!decltype(general)::value) base = both(fmaf(step_slope, (float)(kv0 + col - q), add));
+                uint64_t a = both(add);
+                if constexpr (kSlope && !decltype(general)::value) {
+                    const float at = fmaf(step_slope, (float)(kv0 + col - q), add);
+                    a = pack_f32x2(at, at + step_slope);
+                }
 #pragma unroll
                 for (int i = 0; i < 8; i += 2) {
                     const uint64_t raw = pack_u32x2(sr[i], sr[i + 1]);
-                    uint64_t a = base, y;
-                    if constexpr (kSlope)
-                        if constexpr (!decltype(general)::value) a = add_f32x2(base, pack_f32x2(step_slope * (float)i, step_slope * (float)(i + 1)));
+                    uint64_t y;
+                    if constexpr (kSlope && !decltype(general)::value)
+                        if (i > 0) a = add_f32x2(a, both(2.0f * step_slope));
                     if constexpr (kCap && decltype(general)::value) {
                         float u0, u1, a0, a1;
                         unpack_f32x2(mul_f32x2(raw, to_tanh2), u0, u1);
