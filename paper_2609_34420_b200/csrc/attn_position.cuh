@@ -34,6 +34,20 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8])
                  ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
 
+// 32 bytes, a whole sector, in one store where the address allows it (`whole`: of all that a kernel writes): 32 lanes that each write a row of
+// their own in pieces of 16 bytes send every sector to the L2 twice.
+__device__ __forceinline__ void store_sector(void* at, bool whole, const uint32_t (&w)[8])
+{
+    if (whole)
+        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                     ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+    else {
+        ((uint4*)at)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        ((uint4*)at)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+}
+inline bool whole_sectors(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31u) == 0; }
+
 // P(u) of two arguments u = y^2.
 __device__ __forceinline__ uint64_t tanh_ratio(uint64_t u)
 {

@@ -64,6 +64,7 @@ struct PositionBwdParams {
     int32_t n_heads;
     int32_t group;           // query heads per key head
     int32_t causal;
+    int32_t whole;           // rows of dk and dv begin at whole sectors
     int32_t early_release;   // let the next kernel start its set-up while this one runs
     float c1;                // log2(e) / sqrt(d)
     float scale;             // 1 / sqrt(d)
@@ -616,15 +617,13 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             } else {
                 const float mul = half == 0 ? 1.0f : p.scale;
                 __nv_bfloat16* row = half == 0 ? p.dv + (int64_t)node * p.dv_row : p.dk + (int64_t)node * p.dk_row;
-                uint4* dst = (uint4*)(row + kv_head * D + ch * kOC);
+                __nv_bfloat16* dst = row + kv_head * D + ch * kOC;
 #pragma unroll
-                for (int e = 0; e < kOC / 8; ++e) {
-                    uint4 v;
-                    v.x = pack_bf16x2(__uint_as_float(o[8 * e]) * mul, __uint_as_float(o[8 * e + 1]) * mul);
-                    v.y = pack_bf16x2(__uint_as_float(o[8 * e + 2]) * mul, __uint_as_float(o[8 * e + 3]) * mul);
-                    v.z = pack_bf16x2(__uint_as_float(o[8 * e + 4]) * mul, __uint_as_float(o[8 * e + 5]) * mul);
-                    v.w = pack_bf16x2(__uint_as_float(o[8 * e + 6]) * mul, __uint_as_float(o[8 * e + 7]) * mul);
-                    dst[e] = v;
+                for (int e = 0; e < kOC; e += 16) {
+                    uint32_t w[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[i] = pack_bf16x2(__uint_as_float(o[e + 2 * i]) * mul, __uint_as_float(o[e + 2 * i + 1]) * mul);
+                    store_sector(dst + e, p.whole, w);
                 }
             }
         }
@@ -914,6 +913,7 @@ extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const vo
     p.dv = (__nv_bfloat16*)dv;
     p.dk_row = row[4];
     p.dv_row = row[5];
+    p.whole = position::whole_sectors(dk) && position::whole_sectors(dv) && row[4] % 16 == 0 && row[5] % 16 == 0;
     p.parts = batch->n_graphs > 1 && list_saves(batch, kTile, n_heads, 0) ? 1 : parts_of(batch, n_heads, n_kv_heads, head_dim, causal != 0);
     const bool sums = n_heads > n_kv_heads || p.parts > 1;
     if (sums) {

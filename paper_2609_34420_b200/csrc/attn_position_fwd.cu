@@ -67,6 +67,7 @@ struct PositionFwdParams {
     int32_t n_heads;
     int32_t group;             // query heads per key head
     int32_t causal;
+    int32_t whole;             // out and out_f32 begin at a whole sector
     int32_t early_release;     // let the next kernel start its set-up while this one runs
     float c1;                  // log2(e) / sqrt(d)
     float to_tanh;             // 1 / (sqrt(d) cap)
@@ -672,19 +673,25 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             if constexpr (kExact) {
 #pragma unroll
                 for (int i = 0; i < kOC; ++i) x[i] = __uint_as_float(o[i]) / l_rounded;      // (a row with one key gets that key's value to the bit)
-                float4* dst32 = (float4*)(p.out_f32 + ((size_t)node * p.n_heads + h) * D + hf * kOC);
+                float* dst32 = p.out_f32 + ((size_t)node * p.n_heads + h) * D + hf * kOC;
 #pragma unroll
-                for (int i = 0; i < kOC / 4; ++i) dst32[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+                for (int i = 0; i < kOC; i += 8) {
+                    const uint32_t w[8] = {__float_as_uint(x[i]), __float_as_uint(x[i + 1]), __float_as_uint(x[i + 2]), __float_as_uint(x[i + 3]),
+                                           __float_as_uint(x[i + 4]), __float_as_uint(x[i + 5]), __float_as_uint(x[i + 6]), __float_as_uint(x[i + 7])};
+                    store_sector(dst32 + i, p.whole, w);
+                }
             } else {
                 const float inv_l = 1.0f / l;
 #pragma unroll
                 for (int i = 0; i < kOC; ++i) x[i] = __uint_as_float(o[i]) * inv_l;
             }
-            uint4* dst = (uint4*)(p.out + ((size_t)node * p.n_heads + h) * D + hf * kOC);
+            __nv_bfloat16* dst = p.out + ((size_t)node * p.n_heads + h) * D + hf * kOC;
 #pragma unroll
-            for (int i = 0; i < kOC / 8; ++i)
-                dst[i] = make_uint4(pack_bf16x2(x[8 * i], x[8 * i + 1]), pack_bf16x2(x[8 * i + 2], x[8 * i + 3]), pack_bf16x2(x[8 * i + 4], x[8 * i + 5]),
-                                    pack_bf16x2(x[8 * i + 6], x[8 * i + 7]));
+            for (int i = 0; i < kOC; i += 16) {
+                const uint32_t w[8] = {pack_bf16x2(x[i], x[i + 1]), pack_bf16x2(x[i + 2], x[i + 3]), pack_bf16x2(x[i + 4], x[i + 5]), pack_bf16x2(x[i + 6], x[i + 7]),
+                                       pack_bf16x2(x[i + 8], x[i + 9]), pack_bf16x2(x[i + 10], x[i + 11]), pack_bf16x2(x[i + 12], x[i + 13]), pack_bf16x2(x[i + 14], x[i + 15])};
+                store_sector(dst + i, p.whole, w);
+            }
             if (hf == 0) p.lse[(size_t)h * p.n_total + node] = (m + log2f(l)) * kLn2;
         }
         }
@@ -778,6 +785,7 @@ extern "C" gt_status gt_position_attn_fwd(const void* q, const void* k, const vo
     p.slopes = slopes;
     p.out = (__nv_bfloat16*)out;
     p.out_f32 = out_f32;
+    p.whole = position::whole_sectors(out) && position::whole_sectors(out_f32);
     p.lse = lse;
     p.status = (uint32_t*)workspace;
     p.next_item = (uint32_t*)workspace + kNextForward;
