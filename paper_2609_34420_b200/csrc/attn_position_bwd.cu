@@ -78,7 +78,7 @@ enum Barrier {
     kBarKFull = kBarItemEmpty + 2,           // [2]  K of an item
     kBarKEmpty = kBarKFull + 2,              // [2]  commit behind the item's last dQ MMA
     kBarVFull = kBarKEmpty + 2,              //      V of an item
-    kBarVEmpty,                              //      4 warp arrivals: V rows copied to tensor memory
+    kBarVEmpty,                              //      4 warp arrivals, V rows copied to tensor memory; commit behind the item's first dP^T MMAs
     kBarQdoFull,                             // [2]  Q_i, dO_i and the per-query rows of tile i
     kBarStageEmpty = kBarQdoFull + kStages,  // [2]  commits behind the last MMAs that read Q_i / dO_i
     kBarSFull = kBarStageEmpty + kStages,    // [2]  per half: S^T of the next tile is in tensor memory
@@ -88,6 +88,7 @@ enum Barrier {
     kBarDqFull = kBarDsReady + 2,
     kBarDqFree,
     kBarKvTmem,                              //      8 warp arrivals: K and V rows copied to tensor memory
+    kBarKvDone,                              //      commits behind the item's last S^T and dP^T MMAs, which read them there
     kBarQClear,                              //      the rows of a Q and a dO tile behind the document are cleared
     kBarFinal,                               //      dV and dK of an item
     kBarAccFree,                             //      16 warp arrivals: they have been read
@@ -163,10 +164,11 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             mbar_init(bar(kBarDsReady + s), kSoftmaxWarps / 2);
         }
         mbar_init(bar(kBarVFull), 1);
-        mbar_init(bar(kBarVEmpty), 4);
+        mbar_init(bar(kBarVEmpty), 5);
         mbar_init(bar(kBarDqFull), 1);
         mbar_init(bar(kBarDqFree), 4);
         mbar_init(bar(kBarKvTmem), 8);
+        mbar_init(bar(kBarKvDone), 2);
         mbar_init(bar(kBarQClear), 1);
         mbar_init(bar(kBarFinal), 2);
         mbar_init(bar(kBarAccFree), kSoftmaxWarps);
@@ -308,14 +310,22 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             const uint32_t reg_off = on_p ? 0 : kHalf;          // S^T/P^T or dP^T/dS^T part of a TMEM stage
             const uint32_t in_a_col = on_p ? kColK : kColV;
             const int bar_ready = on_p ? kBarPReady : kBarDsReady, bar_full = on_p ? kBarSFull : kBarDpFull;
-            auto issue_input = [&](int c, int sub) {            // (S^T - lse sqrt(d)) or (dP^T - Delta) of a half tile
+            // (S^T - lse sqrt(d)) or (dP^T - Delta) of a half tile.  An item's first tile takes K and V from shared memory: it can go while the
+            // softmax warps are still at the item before.
+            auto issue_input = [&](int c, int sub, int k, bool begins) {
                 const int s = c & 1;
                 const uint64_t db = make_smem_desc(smem_u32(smem + in_b_off + s * L::kStageBytes) + sub * kHalf * L::kRowBytes, L::kRowBytes, 0);
                 const uint64_t dext = make_smem_desc(smem_u32(smem + L::kExt + s * kExtTileBytes) + sub * kHalf * kExtCols * 2, kExtCols * 2, 0);
                 const uint32_t d = tm + sub * 128 + reg_off;
+                if (begins) {
+                    const uint64_t da = make_smem_desc(smem_u32(smem + (on_p ? L::kK + (k & 1) * L::kTileBytes : L::kV)), L::kRowBytes, 0);
 #pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks)             // A = K or V from tensor memory: 8 packed columns per K step
-                    mma_ts(d, tm + in_a_col + ks * 8, advance_desc(db, ks * 32), idesc_in, ks > 0);
+                    for (int ks = 0; ks < D / 16; ++ks) mma_ss(d, advance_desc(da, ks * 32), advance_desc(db, ks * 32), idesc_in, ks > 0);
+                } else {
+#pragma unroll
+                    for (int ks = 0; ks < D / 16; ++ks)         // A = K or V from tensor memory: 8 packed columns per K step
+                        mma_ts(d, tm + in_a_col + ks * 8, advance_desc(db, ks * 32), idesc_in, ks > 0);
+                }
                 if (!kCap || !on_p) mma_ss(d, desc_ones, dext, idesc_in, 1u);
                 mma_commit(bar(bar_full + sub));
             };
@@ -328,10 +338,18 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     mbar_wait(bar(kBarQdoFull + ((c + i) & 1)), ((c + i) >> 1) & 1, abort_flag, p.status, 321);
                     if (ragged && i == n_q - 1) mbar_wait(bar(kBarQClear), cleared & 1, abort_flag, p.status, 322);
                 };
-                mbar_wait(bar(kBarKvTmem), k & 1, abort_flag, p.status, 320);
+                if (on_p) mbar_wait(bar(kBarKFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 325);
+                else mbar_wait(bar(kBarVFull), k & 1, abort_flag, p.status, 326);
                 wait_tile(0);
                 tc_fence_after();
-                if (elect_one()) { issue_input(c, 0); issue_input(c, 1); }
+                if (elect_one()) {
+                    issue_input(c, 0, k, true);
+                    issue_input(c, 1, k, true);
+                    if (!on_p) mma_commit(bar(kBarVEmpty));
+                }
+                __syncwarp();
+                mbar_wait(bar(kBarKvTmem), k & 1, abort_flag, p.status, 320);
+                if (n_q == 1 && elect_one()) mma_commit(bar(kBarKvDone));
                 __syncwarp();
                 if (k > 0) mbar_wait(bar(kBarAccFree), (k - 1) & 1, abort_flag, p.status, 324);
                 bool acc_started = false;           // the first MMA into the accumulator overwrites it
@@ -353,7 +371,8 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                                 mma_commit(bar(kBarStageEmpty + s));    // this issuer's reads of Q_i / dO_i are done (the other one commits too)
                                 if (i + 1 == n_q) mma_commit(bar(kBarFinal));
                             }
-                            if (i + 1 < n_q) issue_input(c + i + 1, sub);
+                            if (i + 1 < n_q) issue_input(c + i + 1, sub, k, false);
+                            if (i + 2 == n_q && sub == 1) mma_commit(bar(kBarKvDone));
                         }
                         __syncwarp();
                         acc_started = true;
@@ -420,10 +439,10 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         uint8_t* ds_row = smem + L::kDs + half * 16384 + r * 128;
 
         // K (warps 4-7) and V (warps 8-11) rows of item k -> tensor memory, where they stay as the A operands of S^T = K Q^T and
-        // dP^T = V dO^T, once all MMAs that read the last item's there are done (c: query tiles so far; both halves of the last one)
-        auto copy_kv = [&](int k, int c) {
+        // dP^T = V dO^T, once all MMAs that read the last item's there are done
+        auto copy_kv = [&](int k) {
             if (warp >= 12) return;
-            if (c > 0) mbar_wait(bar((warp < 8 ? kBarSFull : kBarDpFull) + 1), (c - 1) & 1, abort_flag, p.status, 345);
+            if (k > 0) mbar_wait(bar(kBarKvDone), (k - 1) & 1, abort_flag, p.status, 345);
             if (warp < 8) mbar_wait(bar(kBarKFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 344);
             else mbar_wait(bar(kBarVFull), k & 1, abort_flag, p.status, 346);
             tc_fence_after();
@@ -447,7 +466,7 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         };
 
         int c = 0;                                      // query tiles so far
-        if (take(0)) copy_kv(0, 0);
+        if (take(0)) copy_kv(0);
         for (int k = 0; items[k & 1].n > 0 && *abort_flag == 0u; ++k) {
         const int32_t n = items[k & 1].n, q_lo = items[k & 1].q_lo;
         const int32_t key = items[k & 1].kv0 + r, key0 = key - lane;                        // this thread's key, the warp's first one
@@ -488,58 +507,69 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             // ---------------- P^T = exp2((S^T - lse sqrt(d)) c1), or exp2(cap log2(e) tanh(S^T / cap) - lse log2(e)) ----------------
             float top_u = 0.f;
             auto probabilities = [&](auto masked_, auto general) {        // general: any score, any distance
-                uint32_t sv[32];
-                tmem_ld32(tS, sv);
-                tmem_wait_ld();
+                uint32_t sa[16], sb[16];
+                tmem_ld16(tS, sa);
+                [[maybe_unused]] const float ahead = (float)(q0 - key);         // the first query's distance
+                [[maybe_unused]] uint64_t away = pack_f32x2(step_slope * ahead, fmaf(step_slope, ahead, step_slope));
+                auto chunk = [&](int rnd, const uint32_t (&sv)[16]) {
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) {
-                    uint64_t add = both(0.f), x;
-                    if constexpr (kCap) {
-                        const float2 nl = *(const float2*)(s_lse + e);
-                        add = pack_f32x2(nl.x, nl.y);
-                    }
-                    if constexpr (kSlope) {
-                        if constexpr (decltype(general)::value) add = add_f32x2(add, pack_f32x2(-slope2 * fabsf((float)(q0 + e - key)), -slope2 * fabsf((float)(q0 + e + 1 - key))));
-                        else add = fma_f32x2(both(step_slope), pack_f32x2((float)(q0 + e - key), (float)(q0 + e + 1 - key)), add);
-                    }
-                    const uint64_t raw = pack_u32x2(sv[e], sv[e + 1]);
-                    [[maybe_unused]] uint64_t t;
-                    if constexpr (kCap) {
-                        const uint64_t u = mul_f32x2(raw, to_tanh2);
-                        if constexpr (decltype(general)::value) {
-                            float u0, u1;
-                            unpack_f32x2(u, u0, u1);
-                            t = pack_f32x2(tanh_any(u0), tanh_any(u1));
-                        } else {
-                            const uint64_t uu = mul_f32x2(u, u);
-                            float u0, u1;
-                            unpack_f32x2(uu, u0, u1);
-                            top_u = max3(top_u, u0, u1);
-                            t = mul_f32x2(u, tanh_ratio(uu));
+                    for (int i = 0; i < 16; i += 2) {
+                        const int e = rnd * 16 + i;
+                        [[maybe_unused]] uint64_t add = both(0.f), t;
+                        uint64_t x;
+                        if constexpr (kCap) {
+                            const float2 nl = *(const float2*)(s_lse + e);
+                            add = pack_f32x2(nl.x, nl.y);
                         }
-                        x = fma_f32x2(t, cap22, add);
-                    } else if constexpr (kSlope) {
-                        x = fma_f32x2(raw, c1c1, add);
-                    } else {
-                        x = mul_f32x2(raw, c1c1);
+                        if constexpr (kSlope && decltype(general)::value) {
+                            add = add_f32x2(add, pack_f32x2(-slope2 * fabsf(ahead + (float)e), -slope2 * fabsf(ahead + (float)(e + 1))));
+                        } else if constexpr (kSlope) {
+                            if (e > 0) away = add_f32x2(away, both(2.0f * step_slope));
+                            add = kCap ? add_f32x2(add, away) : away;
+                        }
+                        const uint64_t raw = pack_u32x2(sv[i], sv[i + 1]);
+                        if constexpr (kCap) {
+                            const uint64_t u = mul_f32x2(raw, to_tanh2);
+                            float u0, u1;
+                            if constexpr (decltype(general)::value) {
+                                unpack_f32x2(u, u0, u1);
+                                t = pack_f32x2(tanh_any(u0), tanh_any(u1));
+                            } else {
+                                const uint64_t uu = mul_f32x2(u, u);
+                                unpack_f32x2(uu, u0, u1);
+                                top_u = max3(top_u, u0, u1);
+                                t = mul_f32x2(u, tanh_ratio(uu));
+                            }
+                            x = fma_f32x2(t, cap22, add);
+                        } else if constexpr (kSlope) {
+                            x = fma_f32x2(raw, c1c1, add);
+                        } else {
+                            x = mul_f32x2(raw, c1c1);
+                        }
+                        float lo, hi;
+                        unpack_f32x2(x, lo, hi);
+                        lo = ex2_approx(lo);
+                        hi = ex2_approx(hi);
+                        if constexpr (decltype(masked_)::value) {
+                            if (e < c_from || e >= c_to) lo = 0.f;
+                            if (e + 1 < c_from || e + 1 >= c_to) hi = 0.f;
+                        }
+                        pk[e >> 1] = pack_bf16x2(lo, hi);
+                        if constexpr (kCap) {
+                            const uint64_t minus = mul_f32x2(t, both(-1.f));
+                            unpack_f32x2(mul_f32x2(pack_f32x2(lo, hi), fma_f32x2(minus, t, both(1.f))), pr[e], pr[e + 1]);
+                        } else {
+                            pr[e] = lo;
+                            pr[e + 1] = hi;
+                        }
                     }
-                    float lo, hi;
-                    unpack_f32x2(x, lo, hi);
-                    lo = ex2_approx(lo);
-                    hi = ex2_approx(hi);
-                    if constexpr (decltype(masked_)::value) {
-                        if (e < c_from || e >= c_to) lo = 0.f;
-                        if (e + 1 < c_from || e + 1 >= c_to) hi = 0.f;
-                    }
-                    pk[e >> 1] = pack_bf16x2(lo, hi);
-                    if constexpr (kCap) {
-                        const uint64_t minus = mul_f32x2(t, both(-1.f));
-                        unpack_f32x2(mul_f32x2(pack_f32x2(lo, hi), fma_f32x2(minus, t, both(1.f))), pr[e], pr[e + 1]);
-                    } else {
-                        pr[e] = lo;
-                        pr[e + 1] = hi;
-                    }
-                }
+                };
+                if constexpr (!kCap) tmem_ld16(tS + 16, sb);
+                tmem_wait_ld();
+                if constexpr (kCap) tmem_ld16(tS + 16, sb);      // (fewer registers at a time)
+                chunk(0, sa);
+                if constexpr (kCap) tmem_wait_ld();
+                chunk(1, sb);
             };
             if (mixed) probabilities(Tag<true>{}, Tag<true>{});
             else {
@@ -595,7 +625,7 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         }
 
         // ---------------- the next item's K and V, then dV (first half's warps) and dK (second half's) ----------------
-        if (take(k + 1)) copy_kv(k + 1, c);
+        if (take(k + 1)) copy_kv(k + 1);
         mbar_wait(bar(kBarFinal), k & 1, abort_flag, p.status, 343);
         tc_fence_after();
         constexpr int kOC = D / 2;                  // output columns per thread

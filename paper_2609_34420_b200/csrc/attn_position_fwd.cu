@@ -441,7 +441,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             // a distance is made for every element.
             const bool before = kv0 + kCols - 1 <= row0 || (p.causal && kv0 >= prefix), behind = kv0 >= row0 + 31;
             [[maybe_unused]] const bool mixed = kSlope && !before && !behind;
-            [[maybe_unused]] const float step_slope = before ? slope2 : -slope2;
+            [[maybe_unused]] const float step_slope = before ? slope2 : -slope2, ahead = (float)(kv0 - q);       // ahead: the first key's distance
             [[maybe_unused]] uint32_t pk[32];      // P of this thread's columns, bf16 pairs
             float tile_sum = 0.f;
             [[maybe_unused]] uint64_t rounded2 = 0;
@@ -456,7 +456,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 for (int i = 0; i < 4; ++i) {
                     float x = __uint_as_float(sa[4 * i]) * p.c1;
                     if constexpr (kCap) x = fminf(fmaxf(x, -p.cap2), p.cap2);
-                    if constexpr (kSlope) x -= slope2 * fabsf((float)(kv0 + 4 * i - q));
+                    if constexpr (kSlope) x -= slope2 * fabsf(ahead + (float)(4 * i));
                     if (4 * i < valid) top = fmaxf(top, x);
                 }
                 exact = named_barrier_or(pair_bar, 64, valid > 0 && counts && !(fabsf(top) <= kPeekReach));   // (a half without valid columns has no say)
@@ -467,7 +467,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             auto scores8 = [&](const uint32_t* sr, int col, float add, auto rag, auto general, float (&x)[8]) {
                 uint64_t a = both(add);
                 if constexpr (kSlope && !decltype(general)::value) {
-                    const float at = fmaf(step_slope, (float)(kv0 + col - q), add);
+                    const float at = fmaf(step_slope, ahead + (float)col, add);
                     a = pack_f32x2(at, at + step_slope);
                 }
 #pragma unroll
@@ -497,8 +497,8 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     unpack_f32x2(y, x[i], x[i + 1]);
                     if constexpr (kSlope)
                         if constexpr (decltype(general)::value) {
-                            x[i] = fmaf(-slope2, fabsf((float)(kv0 + col + i - q)), x[i]);
-                            x[i + 1] = fmaf(-slope2, fabsf((float)(kv0 + col + i + 1 - q)), x[i + 1]);
+                            x[i] = fmaf(-slope2, fabsf(ahead + (float)(col + i)), x[i]);
+                            x[i + 1] = fmaf(-slope2, fabsf(ahead + (float)(col + i + 1)), x[i + 1]);
                         }
                 }
             };
