@@ -56,9 +56,11 @@ struct PositionBwdParams {
     float* dv_acc;
     uint32_t* status;
     uint32_t* next_item;     // counts the items that have been taken beyond the grid's first ones; 0 before and after the kernel
-    const int4* list;        // packed batch: work list; item = entry * heads + head (nullptr: heads, then documents, then tiles)
+    const int4* list;        // packed batch: work list; item = entry * heads + head (nullptr: heads, then documents and tiles)
     int32_t n_items;
     int32_t parts;           // without a list: items that share the queries of a key tile (then dk_acc and dv_acc are used)
+    int32_t by_work;         // without a list: the same tile of all documents, then the next (else document after document)
+    int32_t blocks;          // ... of the longest document
     int32_t n_graphs;
     int32_t n_total;
     int32_t n_heads;
@@ -240,8 +242,8 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         int32_t row = index / p.n_heads;
                         part = row % p.parts;
                         row /= p.parts;
-                        tile = row / p.n_graphs;
-                        g = row % p.n_graphs;
+                        tile = p.by_work ? row / p.n_graphs : row % p.blocks;
+                        g = p.by_work ? row % p.n_graphs : row / p.blocks;
                         item.node0 = p.cu_seqlens ? p.cu_seqlens[g] : 0;
                         item.n = p.cu_seqlens ? p.cu_seqlens[g + 1] - item.node0 : p.n_total;
                     }
@@ -953,6 +955,8 @@ extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const vo
     p.status = (uint32_t*)workspace;
     p.next_item = (uint32_t*)workspace + kNextBackward;
     p.n_graphs = batch->n_graphs;
+    p.blocks = (batch->max_seqlen + kTile - 1) / kTile;
+    p.by_work = batch->n_graphs == 1 || list_by_work(batch, causal, (size_t)T * n_heads * head_dim * 8);
     int64_t n_items = (int64_t)((batch->max_seqlen + kTile - 1) / kTile) * batch->n_graphs * n_heads * p.parts;
     if (batch->n_graphs > 1 && list_saves(batch, kTile, n_heads, 0)) {
         p.list = (const int4*)(ws + w.list_off);
@@ -983,7 +987,7 @@ extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const vo
     pre.n_total = T;
     pre.n_graphs = batch->n_graphs;
     pre.n_heads = n_heads;
-    pre.by_work = list_by_work(batch, causal, (size_t)T * n_heads * head_dim * 8);
+    pre.by_work = p.by_work;
     pre.row_blocks = (uint32_t)(((size_t)T * n_heads + kPrepareRows - 1) / kPrepareRows);
     pre.sqrt_d = sqrtf((float)head_dim);
     const uint32_t list_blocks = p.list ? (uint32_t)((batch->n_graphs + kPrepareThreads / 32 - 1) / (kPrepareThreads / 32)) : 0;

@@ -59,9 +59,11 @@ struct PositionFwdParams {
     float* lse;                // [H,T]
     uint32_t* status;
     uint32_t* next_item;       // counts the items that have been taken beyond the grid's first ones; 0 before and after the kernel
-    const int4* list;          // packed batch: work list; item = entry * heads + head (nullptr: heads, then documents, then blocks)
+    const int4* list;          // packed batch: work list; item = entry * heads + head (nullptr: heads, then documents and blocks)
     int32_t n_items;
     int32_t halves_from;       // without a list: rows of items (all heads of a block) from this one on are halved
+    int32_t by_work;           // without a list: the same block of all documents, then the next (else document after document)
+    int32_t blocks;            // ... of the longest document
     int32_t n_graphs;
     int32_t n_total;
     int32_t n_heads;
@@ -235,8 +237,8 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                             part = (row - p.halves_from) & 1;
                             row = p.halves_from + (row - p.halves_from) / 2;
                         }
-                        block = row / p.n_graphs;
-                        g = row % p.n_graphs;
+                        block = p.by_work ? row / p.n_graphs : row % p.blocks;
+                        g = p.by_work ? row % p.n_graphs : row / p.blocks;
                         item.node0 = p.cu_seqlens ? p.cu_seqlens[g] : 0;
                         item.n = p.cu_seqlens ? p.cu_seqlens[g + 1] - item.node0 : p.n_total;
                     }
@@ -800,6 +802,8 @@ extern "C" gt_status gt_position_attn_fwd(const void* q, const void* k, const vo
     p.n_graphs = batch->n_graphs;
     const int32_t rows = one_tile_blocks(batch, n_heads, causal != 0) ? kTile : 2 * kTile;
     const int32_t blocks = (batch->max_seqlen + rows - 1) / rows;
+    p.blocks = blocks;
+    p.by_work = batch->n_graphs == 1 || list_by_work(batch, causal, (size_t)batch->n_total * n_kv_heads * head_dim * 4);
     int64_t n_items = (int64_t)blocks * batch->n_graphs * n_heads;
     p.halves_from = blocks * batch->n_graphs;
     if (rows == 2 * kTile && batch->n_graphs == 1 && !causal) {
@@ -813,7 +817,7 @@ extern "C" gt_status gt_position_attn_fwd(const void* q, const void* k, const vo
         n_items = (int64_t)list_entries(batch, rows) * n_heads;
         const unsigned blocks = (unsigned)((batch->n_graphs + kListThreads / 32 - 1) / (kListThreads / 32));
         if ((st = launch_overlapped(position_list_kernel, dim3(blocks), kListThreads, 0, s, list, (int32_t)list_entries(batch, rows), batch->cu_seqlens,
-                                    batch->n_graphs, list_by_work(batch, causal, (size_t)batch->n_total * n_kv_heads * head_dim * 4))) != GT_OK)
+                                    batch->n_graphs, p.by_work != 0)) != GT_OK)
             return st;
     }
     if (n_items > 0x7fff0000) return GT_ERR_UNSUPPORTED;
