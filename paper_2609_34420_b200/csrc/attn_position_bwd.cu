@@ -19,7 +19,7 @@
 //   warps 1, 3, 2 MMA issuers: dV and the next S^T; dK and the next dP^T; dQ (which also clears what lies behind the document)
 //   warps 4-19    softmax: warps 4-11 own queries [0,64) of every tile, warps 12-19 queries [64,128); within a half, four warps per 32
 //                 query columns
-//   warps 20-23   dQ reducer: TMEM -> shared memory -> TMA reduce-add into the fp32 accumulator
+//   warps 20-23   dQ reducer: TMEM -> shared memory -> TMA reduce-add into the fp32 accumulator; dV and dK of an item
 //
 // TMEM columns, half g: S^T/P^T [128g, 128g+64)  dP^T/dS^T [128g+64, 128g+128);
 //               dV [256,320)  dK [320,384)  dQ [384,448)  K [448,480)  V [480,512) (bf16 pairs).
@@ -93,7 +93,7 @@ enum Barrier {
     kBarKvDone,                              //      commits behind the item's last S^T and dP^T MMAs, which read them there
     kBarQClear,                              //      the rows of a Q and a dO tile behind the document are cleared
     kBarFinal,                               //      dV and dK of an item
-    kBarAccFree,                             //      16 warp arrivals: they have been read
+    kBarAccFree,                             //      4 warp arrivals: they have been read
     kNumBarriers
 };
 constexpr int kNbDqStaged = 4, kNbDqStagingFree = 5;       // named barriers
@@ -173,7 +173,7 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         mbar_init(bar(kBarKvDone), 2);
         mbar_init(bar(kBarQClear), 1);
         mbar_init(bar(kBarFinal), 2);
-        mbar_init(bar(kBarAccFree), kSoftmaxWarps);
+        mbar_init(bar(kBarAccFree), 4);
         fence_mbar_init();
         prefetch_tensormap(&tmap_q);
         prefetch_tensormap(&tmap_k);
@@ -468,8 +468,8 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         };
 
         int c = 0;                                      // query tiles so far
-        if (take(0)) copy_kv(0);
-        for (int k = 0; items[k & 1].n > 0 && *abort_flag == 0u; ++k) {
+        for (int k = 0; take(k); ++k) {
+        copy_kv(k);
         const int32_t n = items[k & 1].n, q_lo = items[k & 1].q_lo;
         const int32_t key = items[k & 1].kv0 + r, key0 = key - lane;                        // this thread's key, the warp's first one
         // queries [from, to) see the key
@@ -485,6 +485,7 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         };
         [[maybe_unused]] float next_lse = kCap ? fetch_lse(0) : 0.f;
         const int n_q = items[k & 1].q_tiles();
+        give_back(k);
 
         for (int i = 0; i < n_q; ++i, ++c) {
             const int32_t q0 = q_lo + i * kTile + grp * 32;                     // the group's first query
@@ -626,40 +627,6 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             if (lane == 0) mbar_arrive(bar(kBarDsReady + half));
         }
 
-        // ---------------- the next item's K and V, then dV (first half's warps) and dK (second half's) ----------------
-        if (take(k + 1)) copy_kv(k + 1);
-        mbar_wait(bar(kBarFinal), k & 1, abort_flag, p.status, 343);
-        tc_fence_after();
-        constexpr int kOC = D / 2;                  // output columns per thread
-        const int ch = grp & 1;
-        const uint32_t tacc = tmem + (half == 0 ? kColDv : kColDk) + ch * kOC + lane_off;
-        uint32_t o[kOC];
-        if constexpr (kOC == 32) tmem_ld32(tacc, o); else tmem_ld16(tacc, o);
-        tmem_wait_ld();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(kBarAccFree));
-        if (key < n) {
-            const int32_t node = items[k & 1].node0 + key, kv_head = items[k & 1].head / p.group;
-            if (p.dk_acc != nullptr) {
-                const size_t at = ((size_t)node * (p.n_heads / p.group) + kv_head) * D + ch * kOC;
-                float4* dst = (float4*)((half == 0 ? p.dv_acc : p.dk_acc) + at);
-#pragma unroll
-                for (int e = 0; e < kOC / 4; ++e) red_add_f32x4(dst + e, o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
-            } else {
-                const float mul = half == 0 ? 1.0f : p.scale;
-                __nv_bfloat16* row = half == 0 ? p.dv + (int64_t)node * p.dv_row : p.dk + (int64_t)node * p.dk_row;
-                __nv_bfloat16* dst = row + kv_head * D + ch * kOC;
-#pragma unroll
-                for (int e = 0; e < kOC; e += 16) {
-                    uint32_t w[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) w[i] = pack_bf16x2(__uint_as_float(o[e + 2 * i]) * mul, __uint_as_float(o[e + 2 * i + 1]) * mul);
-                    store_sector(dst + e, p.whole, w);
-                }
-            }
-        }
-        give_back(k);
         }
     } else {
         // ================================ dQ reducer ================================
@@ -673,7 +640,6 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         for (int k = 0; take(k); ++k) {
             const int n_q = items[k & 1].q_tiles();
             const int32_t n_own = items[k & 1].n - items[k & 1].q_lo, row0 = items[k & 1].node0 + items[k & 1].q_lo, col0 = items[k & 1].head * D;
-            give_back(k);
             for (int i = 0; i < n_q; ++i, ++c) {
                 mbar_wait(bar(kBarDqFull), c & 1, abort_flag, p.status, 350);
                 tc_fence_after();
@@ -701,6 +667,33 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         __syncwarp();
                     }
                 }
+            }
+            // The item's dV and dK, from here, so that the softmax warps go on with the next one.
+            const int32_t key = items[k & 1].kv0 + r, node = items[k & 1].node0 + key, kv_head = items[k & 1].head / p.group;
+            const bool mine = key < items[k & 1].n;
+            give_back(k);
+            mbar_wait(bar(kBarFinal), k & 1, abort_flag, p.status, 343);
+            tc_fence_after();
+#pragma unroll
+            for (int e = 0; e < 2 * D; e += 16) {
+                uint32_t o[16];
+                tmem_ld16(tmem + (e < D ? kColDv + e : kColDk + e - D) + lane_off, o);
+                tmem_wait_ld();
+                if (e == 2 * D - 16) { tc_fence_before(); __syncwarp(); if (lane == 0) mbar_arrive(bar(kBarAccFree)); }
+                const int col = e < D ? e : e - D;
+                if (mine && p.dk_acc != nullptr) {
+                    float4* dst = (float4*)((e < D ? p.dv_acc : p.dk_acc) + ((size_t)node * (p.n_heads / p.group) + kv_head) * D + col);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) red_add_f32x4(dst + i, o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                } else if (mine) {
+                    const float mul = e < D ? 1.0f : p.scale;
+                    __nv_bfloat16* row = e < D ? p.dv + (int64_t)node * p.dv_row : p.dk + (int64_t)node * p.dk_row;
+                    uint32_t w[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[i] = pack_bf16x2(__uint_as_float(o[2 * i]) * mul, __uint_as_float(o[2 * i + 1]) * mul);
+                    store_sector(row + kv_head * D + col, p.whole, w);
+                }
+                __syncwarp();
             }
         }
         if (warp == 20 && elect_one()) bulk_wait_group0();      // all adds have landed before the CTA retires
