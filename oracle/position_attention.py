@@ -18,6 +18,26 @@ from __future__ import annotations
 
 import numpy as np
 
+def _rows_times(a, x):
+    """sum_j a[h,i,j] x[j,h,d]."""
+    return np.matmul(a, x.transpose(1, 0, 2)).transpose(1, 0, 2)
+
+
+def _columns_times(a, x):
+    """sum_i a[h,i,j] x[i,h,d]."""
+    return np.matmul(a.transpose(0, 2, 1), x.transpose(1, 0, 2)).transpose(1, 0, 2)
+
+
+def _products(x, y):
+    """sum_c x[i,h,c] y[j,h,c]."""
+    return np.matmul(x.transpose(1, 0, 2), y.transpose(1, 2, 0))
+
+
+def _weighed(a, x):
+    """sum_ij a[h,i,j] sum_d x[i,h,d]."""
+    return (a.sum(2) * x.sum(2).T).sum()
+
+
 HALF_STEP = 2.0 ** -8          # bf16
 MEAN_STEP = HALF_STEP / 3 ** 0.5
 
@@ -27,8 +47,8 @@ def scores(q, k, causal, prefix, slopes, cap):
     n, H, d = q.shape
     kk = np.repeat(k, H // k.shape[1], axis=1)
     with np.errstate(invalid="ignore"):
-        x = np.einsum("ihd,jhd->hij", q, kk) / np.sqrt(d)
-        size = np.einsum("ihd,jhd->hij", np.abs(q), np.abs(kk)) / np.sqrt(d)
+        x = _products(q, kk) / np.sqrt(d)
+        size = _products(np.abs(q), np.abs(kk)) / np.sqrt(d)
     t = np.tanh(x / cap) if cap else np.zeros_like(x)
     s = cap * t if cap else x
     i, j = np.arange(n)[:, None], np.arange(n)[None, :]
@@ -51,21 +71,21 @@ def attention(q, k, v, dout=None, causal=False, prefix=0, slopes=None, cap=0.0):
     e = np.exp(s - top)
     l = e.sum(2, keepdims=True)
     p = e / l
-    out = np.einsum("hij,jhd->ihd", p, vv)
+    out = _rows_times(p, vv)
     lse = (top + np.log(l))[:, :, 0]
     # fp32: products summed in the tensor core (d terms and one for the fold of lse), the tanh's polynomial, exponent and penalty
     slip = 2.0 ** -22 * (d * size + np.abs(lse)[:, :, None]) + 1e-6 * size + 2e-6 + 2.0 ** -21 * np.where(np.isfinite(s), np.abs(s), 0.0)
     drift = (p * slip).sum(2) + 1e-6                       # of a row's log-sum-exp
     wrong = slip + drift[:, :, None]                       # relative, of a probability
-    near = np.einsum("hij,jhd->ihd", p * (HALF_STEP + wrong), np.abs(vv)) * 1.01
+    near = _rows_times(p * (HALF_STEP + wrong), np.abs(vv)) * 1.01
     out32 = near + (HALF_STEP + drift.T[:, :, None]) * np.abs(out)          # (the normaliser is rounded, too, or not)
     r = {"out": out, "lse": lse, "bounds": {"out": out32 + HALF_STEP * np.abs(out) * 1.01, "lse": drift}}
     squares = lambda x: (x * x).sum()  # noqa: E731
     # (the values as they are: their mean over a row is taken off where the normaliser is rounded alike, which can only make it less)
-    r["norms"] = {"out": MEAN_STEP * np.sqrt(np.einsum("hij,jhd->", p * p, vv * vv) + squares(out))}
+    r["norms"] = {"out": MEAN_STEP * np.sqrt(_weighed((p * p).transpose(0, 2, 1), vv * vv) + squares(out))}
     if dout is None:
         return r
-    dp = np.einsum("ihd,jhd->hij", dout, vv)
+    dp = _products(dout, vv)
     delta = (p * dp).sum(2, keepdims=True)
     g = 1.0 - t * t
     dx = p * (dp - delta) * g
@@ -73,24 +93,24 @@ def attention(q, k, v, dout=None, causal=False, prefix=0, slopes=None, cap=0.0):
     def heads(x):
         return x.reshape(n, G, H // G, d).sum(2)
 
-    r["dq"] = np.einsum("hij,jhd->ihd", dx, kk) / np.sqrt(d)
-    r["dk"] = heads(np.einsum("hij,ihd->jhd", dx, q)) / np.sqrt(d)
-    r["dv"] = heads(np.einsum("hij,ihd->jhd", p, dout))
+    r["dq"] = _rows_times(dx, kk) / np.sqrt(d)
+    r["dk"] = heads(_columns_times(dx, q)) / np.sqrt(d)
+    r["dv"] = heads(_columns_times(p, dout))
     b = r["bounds"]
-    sized = np.einsum("ihd,jhd->hij", np.abs(dout), np.abs(vv))
+    sized = _products(np.abs(dout), np.abs(vv))
     tail = 2.0 ** -22 * d * (sized + (np.abs(dout) * np.abs(out)).sum(2).T[:, :, None])
     for key, off in (("", out32), ("_out", b["out"])):
         off_delta = (np.abs(dout) * off).sum(2).T[:, :, None]
         off_x = 1.01 * ((HALF_STEP + wrong) * np.abs(dx) + p * (g + 4e-6) * (off_delta + tail) + p * np.abs(dp - delta) * 4e-6)
-        b["dq" + key] = np.einsum("hij,jhd->ihd", off_x, np.abs(kk)) / np.sqrt(d) + HALF_STEP * 1.01 * np.abs(r["dq"]) + 1e-30
-        b["dk" + key] = heads(np.einsum("hij,ihd->jhd", off_x, np.abs(q))) / np.sqrt(d) + HALF_STEP * 1.01 * np.abs(r["dk"]) + 1e-30
+        b["dq" + key] = _rows_times(off_x, np.abs(kk)) / np.sqrt(d) + HALF_STEP * 1.01 * np.abs(r["dq"]) + 1e-30
+        b["dk" + key] = heads(_columns_times(off_x, np.abs(q))) / np.sqrt(d) + HALF_STEP * 1.01 * np.abs(r["dk"]) + 1e-30
     # Delta with the fp32 output: sum_j of (a probability's rounding) P (dP - Delta), since the rounded normaliser takes the mean off
     off_delta2 = ((p * (dp - delta)) ** 2).sum(2)
-    pull = np.einsum("hij,jhd->ihd", p * g, kk)
-    r["norms"]["dq"] = MEAN_STEP * np.sqrt((np.einsum("hij,jhd->", dx * dx, kk * kk) + (off_delta2.T[:, :, None] * pull * pull).sum()) / d + squares(r["dq"]))
-    r["norms"]["dk"] = MEAN_STEP * np.sqrt(np.einsum("hij,ihd->", dx * dx + (p * g) ** 2 * off_delta2[:, :, None], q * q) / d + squares(r["dk"]))
-    r["norms"]["dv"] = MEAN_STEP * np.sqrt(np.einsum("hij,ihd->", p * p, dout * dout) + squares(r["dv"]))
-    b["dv"] = heads(np.einsum("hij,ihd->jhd", 1.01 * p * (HALF_STEP + wrong), np.abs(dout))) + HALF_STEP * 1.01 * np.abs(r["dv"]) + 1e-30
+    pull = _rows_times(p * g, kk)
+    r["norms"]["dq"] = MEAN_STEP * np.sqrt((_weighed((dx * dx).transpose(0, 2, 1), kk * kk) + (off_delta2.T[:, :, None] * pull * pull).sum()) / d + squares(r["dq"]))
+    r["norms"]["dk"] = MEAN_STEP * np.sqrt(_weighed(dx * dx + (p * g) ** 2 * off_delta2[:, :, None], q * q) / d + squares(r["dk"]))
+    r["norms"]["dv"] = MEAN_STEP * np.sqrt(_weighed(p * p, dout * dout) + squares(r["dv"]))
+    b["dv"] = heads(_columns_times(1.01 * p * (HALF_STEP + wrong), np.abs(dout))) + HALF_STEP * 1.01 * np.abs(r["dv"]) + 1e-30
     return r
 
 

@@ -297,3 +297,69 @@ def test_layer_with_rotary_positions():
     for name, x in (("dq", dq), ("dk", dk)):
         y = opos.rotate(ref[name], f.numpy(), position, False, 1.1, True)
         assert np.linalg.norm(to_f64(x) - y) <= 1.1 * 1.1 * ref["norms"][name] + ONE * np.linalg.norm(y), name          # (turned and scaled by 1.1, rounded once more)
+
+
+def test_results_at_any_16_byte_address():
+    """Results that begin in the middle of a sector; q, k and v, too."""
+    c = Case([200, 77], H=4, G=4, d=32, seed=21)
+
+    def moved(x):
+        return torch.cat([x.new_zeros(8), x.flatten()])[8:].view_as(x)
+
+    for name in ("q", "k", "v", "dout", "out", "dq", "dk", "dv"):
+        setattr(c, name, moved(getattr(c, name)))
+        assert getattr(c, name).data_ptr() % 32 == 16
+    c.out32 = torch.cat([c.out32.new_zeros(4), c.out32.flatten()])[4:].view_as(c.out32)
+    c.run()
+
+
+@pytest.mark.parametrize("options", [dict(), dict(cap=20.0, spread=3.0, slopes=[0.5]), dict(causal=False), dict(cap=200.0, spread=30.0)])
+def test_long_documents_of_few_heads(options):
+    """A persistent block takes several items, queries of a key tile are shared, blocks of one query tile."""
+    Case([2300], H=1, G=1, seed=22, **options).run()
+
+
+def test_more_items_than_blocks():
+    """Every block takes several items, of one and of two query tiles, with and without keys behind the diagonal."""
+    rng = np.random.Generator(np.random.PCG64(7))
+    lengths = [int(n) for n in rng.integers(0, 400, 150)]
+    for options in (dict(), dict(causal=False), dict(prefix=[int(n) for n in rng.integers(0, 400, 150)], cap=30.0, spread=4.0, slopes=[0.1, 0.5, 1.0, 0.0])):
+        Case(lengths, H=4, G=2, d=32, seed=23, **options).run()
+
+
+def test_halved_blocks_of_one_long_document():
+    """All pairs of a document whose last blocks of two query tiles are halved; two rows' results against fp64 by hand."""
+    n, H, d = 5000, 16, 32
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q, k, v = (torch.randn(n, H, d, device="cuda", generator=g).bfloat16() for _ in range(3))
+    out, lse = torch.full_like(q, LEFT), torch.full((H, n), LEFT, device="cuda")
+    gt.gt_check(gt.gt_position_attn_fwd(q, k, v, None, None, gt.Batch(n), False, 0.0, out, lse))
+    x = torch.einsum("ihd,jhd->hij", q.double(), k.double()) / d ** 0.5
+    ref = torch.einsum("hij,jhd->ihd", torch.softmax(x, 2), v.double())
+    assert float((lse.double() - torch.logsumexp(x, 2)).abs().max()) <= 1e-4
+    assert float((out.double() - ref).norm() / ref.norm()) <= 2 * ONE
+
+
+def test_two_calls_at_once_on_two_streams():
+    """With workspaces of their own."""
+    a, b = Case([700, 100, 300], H=4, G=2, seed=24), Case([512, 33], H=8, G=8, cap=10.0, seed=25)
+    torch.cuda.synchronize()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    spaces = []
+    for _ in range(3):
+        for c, s in zip((a, b), streams):
+            with torch.cuda.stream(s):
+                spaces += [c.forward(), c.backward()]
+    torch.cuda.synchronize()
+    for ws in spaces:
+        gt.gt_check(ws)
+    a.check()
+    b.check()
+
+
+def test_counters_are_zero_between_calls():
+    """Words of the workspaces' headers that the persistent kernels count with."""
+    c = Case([300] * 40, H=8, G=8, d=32, seed=26)
+    for ws in (c.forward(), c.backward()):
+        torch.cuda.synchronize()
+        assert not ws[:256].any()
