@@ -69,7 +69,7 @@ struct PositionBwdParams {
     int32_t whole;           // rows of dk and dv begin at whole sectors
     int32_t early_release;   // let the next kernel start its set-up while this one runs
     float c1;                // log2(e) / sqrt(d)
-    float scale;             // 1 / sqrt(d)
+    float ds_scale;          // of dk and dq: 1 / sqrt(d), with a cap its negative
     float to_tanh;           // 1 / (sqrt(d) cap)
     float cap2;              // cap log2(e)
 };
@@ -515,14 +515,15 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 [[maybe_unused]] const float ahead = (float)(q0 - key);         // the first query's distance
                 [[maybe_unused]] uint64_t away = pack_f32x2(step_slope * ahead, fmaf(step_slope, ahead, step_slope));
                 auto chunk = [&](int rnd, const uint32_t (&sv)[16]) {
+                    [[maybe_unused]] float4 nl;
 #pragma unroll
                     for (int i = 0; i < 16; i += 2) {
                         const int e = rnd * 16 + i;
                         [[maybe_unused]] uint64_t add = both(0.f), t;
                         uint64_t x;
                         if constexpr (kCap) {
-                            const float2 nl = *(const float2*)(s_lse + e);
-                            add = pack_f32x2(nl.x, nl.y);
+                            if (e % 4 == 0) nl = *(const float4*)(s_lse + e);
+                            add = e % 4 == 0 ? pack_f32x2(nl.x, nl.y) : pack_f32x2(nl.z, nl.w);
                         }
                         if constexpr (kSlope && decltype(general)::value) {
                             add = add_f32x2(add, pack_f32x2(-slope2 * fabsf(ahead + (float)e), -slope2 * fabsf(ahead + (float)(e + 1))));
@@ -559,8 +560,8 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         }
                         pk[e >> 1] = pack_bf16x2(lo, hi);
                         if constexpr (kCap) {
-                            const uint64_t minus = mul_f32x2(t, both(-1.f));
-                            unpack_f32x2(mul_f32x2(pack_f32x2(lo, hi), fma_f32x2(minus, t, both(1.f))), pr[e], pr[e + 1]);
+                            // -P (1 - tanh^2): the sign goes into the scale of dq and dk
+                            unpack_f32x2(mul_f32x2(pack_f32x2(lo, hi), fma_f32x2(t, t, both(-1.f))), pr[e], pr[e + 1]);
                         } else {
                             pr[e] = lo;
                             pr[e + 1] = hi;
@@ -686,7 +687,7 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 #pragma unroll
                     for (int i = 0; i < 4; ++i) red_add_f32x4(dst + i, o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                 } else if (mine) {
-                    const float mul = e < D ? 1.0f : p.scale;
+                    const float mul = e < D ? 1.0f : p.ds_scale;
                     __nv_bfloat16* row = e < D ? p.dv + (int64_t)node * p.dv_row : p.dk + (int64_t)node * p.dk_row;
                     uint32_t w[8];
 #pragma unroll
@@ -961,9 +962,10 @@ extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const vo
     p.n_heads = n_heads;
     p.group = n_heads / n_kv_heads;
     p.causal = causal != 0;
-    p.scale = 1.0f / sqrtf((float)head_dim);
-    p.c1 = kLog2e * p.scale;
-    p.to_tanh = cap > 0.f ? p.scale / cap : 0.f;
+    const float scale = 1.0f / sqrtf((float)head_dim);
+    p.ds_scale = cap > 0.f ? -scale : scale;
+    p.c1 = kLog2e * scale;
+    p.to_tanh = cap > 0.f ? scale / cap : 0.f;
     p.cap2 = cap * kLog2e;
     cudaStream_t s = (cudaStream_t)stream;
 
@@ -999,7 +1001,7 @@ extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const vo
         f.acc[i] = (const float4*)acc[i];
         f.to[i] = (__nv_bfloat16*)to[i];
         f.row[i] = row[3 + i];
-        f.mul[i] = i < 2 ? p.scale : 1.0f;
+        f.mul[i] = i < 2 ? p.ds_scale : 1.0f;
         f.vecs[i] = (uint32_t)((i == 0 ? n_heads : n_kv_heads) * head_dim / 4);
     }
     f.cu_seqlens = batch->cu_seqlens;

@@ -43,7 +43,7 @@ constexpr int kCW = 16;                       // columns per TMEM load
 constexpr float kSumThreshold = 0x1p24f;       // tile row sum above which the reference is raised
 // Scores of a capped row lie within cap log2(e) of 0 at the diagonal, so that against a reference of half of that the largest P is between 2^-108 and
 // 2^37: sums, products with v of up to 2^60 and their sums stay within fp32, and nothing that counts is lost below.
-constexpr float kBoundedCap = 50.0f;
+constexpr float kBoundedCap = 50.0f, kLeastBoundedCap = 0.01f;       // (below, the scaled coefficients leave fp32)
 // Every eighth pair of exponentials is a polynomial's (ex2_pair), which takes load off the special-function unit (77 % busy without) and adds
 // to the issue slots: 16 384 tokens, 8 heads of 64, all pairs 768 -> 710 us (every sixth 746, every fourth 749, every third 790), causal 372 ->
 // 344, causal with the fp32 output 428 -> 409; with the penalty on distance 411 -> 407, and with both 457 -> 475, so not there.
@@ -75,6 +75,8 @@ struct PositionFwdParams {
     float to_tanh;             // 1 / (sqrt(d) cap)
     float cap2;                // cap log2(e)
     float reference;           // kCapForm 1: of all rows, a whole number
+    float tanh[6];             //   coefficients of tanh(s / cap2) cap2 / s as a polynomial in s^2
+    float reach;               //   s^2 up to which it holds
 };
 
 enum Barrier {
@@ -136,7 +138,7 @@ constexpr int kNbPair = 2;                    // named barriers: + 4 t + lane qu
 __device__ __forceinline__ void setmaxnreg_dec_56() { asm volatile("setmaxnreg.dec.sync.aligned.u32 56;"); }
 
 // kTiles = 1: blocks of one query tile, for grids that would leave half of the SMs idle or more.
-// kCapForm: 0 no cap; 1 a cap of up to kBoundedCap; 2 any cap.  With the second form no score can be out of reach of a reference of half the
+// kCapForm: 0 no cap; 1 a cap of kLeastBoundedCap to kBoundedCap; 2 any cap.  With the second form no score can be out of reach of a reference of half the
 // cap, so that nothing is redone, and P takes the place of the scores chunk by chunk; the registers that this frees are what hides the
 // polynomial's latency (causal 16 384 tokens, cap 30: 665 -> @@ us).
 // kExact (with the fp32 output): O is divided by the sum of the probabilities as the MMA reads them, rounded to bf16, so that their
@@ -466,6 +468,12 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 
             // Scores of eight consecutive columns in log2 units, plus `add`; general: any score, any distance.
             float top_u = 0.f;
+            [[maybe_unused]] auto scaled_ratio = [&](uint64_t u) {
+                uint64_t r = fma_f32x2(both(p.tanh[5]), u, both(p.tanh[4]));
+#pragma unroll
+                for (int i = 3; i >= 0; --i) r = fma_f32x2(r, u, both(p.tanh[i]));
+                return r;
+            };
             auto scores8 = [&](const uint32_t* sr, int col, float add, auto rag, auto general, float (&x)[8]) {
                 uint64_t a = both(add);
                 if constexpr (kSlope && !decltype(general)::value) {
@@ -484,7 +492,8 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         unpack_f32x2(a, a0, a1);
                         y = pack_f32x2(fmaf(p.cap2, tanh_any(u0), a0), fmaf(p.cap2, tanh_any(u1), a1));
                     } else if constexpr (kCap) {
-                        const uint64_t u = mul_f32x2(raw, to_tanh2), uu = mul_f32x2(u, u);
+                        // (kBounded: u is the score itself, in log2 units, and the polynomial's coefficients are made for that)
+                        const uint64_t u = mul_f32x2(raw, kBounded ? c1c1 : to_tanh2), uu = mul_f32x2(u, u);
                         float u0, u1;
                         unpack_f32x2(uu, u0, u1);
                         if constexpr (decltype(rag)::value) {
@@ -492,7 +501,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                             if (col + i + 1 >= valid) u1 = 0.f;
                         }
                         top_u = max3(top_u, u0, u1);
-                        y = fma_f32x2(mul_f32x2(raw, c1c1), tanh_ratio(uu), a);
+                        y = kBounded ? fma_f32x2(u, scaled_ratio(uu), a) : fma_f32x2(mul_f32x2(raw, c1c1), tanh_ratio(uu), a);
                     } else {
                         y = fma_f32x2(raw, c1c1, a);
                     }
@@ -514,7 +523,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     top_u = 0.f;
 #pragma unroll
                     for (int e = 0; e < kCW; e += 8) scores8(sr + e, c * kCW + e, -m, rag, Tag<false>{}, *(float (*)[8])(x + e));
-                    if (__any_sync(0xffffffffu, counts && !(top_u <= kTanhReach)) || mixed) {
+                    if (__any_sync(0xffffffffu, counts && !(top_u <= p.reach)) || mixed) {
 #pragma unroll
                         for (int e = 0; e < kCW; e += 8) scores8(sr + e, c * kCW + e, -m, rag, Tag<true>{}, *(float (*)[8])(x + e));
                     }
@@ -822,8 +831,11 @@ extern "C" gt_status gt_position_attn_fwd(const void* q, const void* k, const vo
     }
     if (n_items > 0x7fff0000) return GT_ERR_UNSUPPORTED;
     p.n_items = (int32_t)n_items;
-    const bool bounded = cap <= kBoundedCap;
+    const bool bounded = cap <= kBoundedCap && cap >= kLeastBoundedCap;
     p.reference = bounded ? floorf(0.5f * p.cap2) : 0.f;
+    const float coefficients[6] = {position::kTanh0, position::kTanh1, position::kTanh2, position::kTanh3, position::kTanh4, position::kTanh5};
+    for (int i = 0; i < 6; ++i) p.tanh[i] = bounded ? (float)(coefficients[i] * std::pow((double)p.cap2, -2.0 * i)) : 0.f;
+    p.reach = position::kTanhReach * p.cap2 * p.cap2;
     auto go = [&](auto wide, auto capped, auto sloped) {
         constexpr int D = decltype(wide)::value ? 64 : 32;
         constexpr bool kCap = decltype(capped)::value, kSlope = decltype(sloped)::value;
