@@ -422,7 +422,7 @@ gt_status gt_feature_code_dweights(const float* dtable, const uint32_t* vectors,
  * over the keys j that i sees: all of its document (causal == 0), or j <= i and j < prefix[g] (causal != 0; prefix int32[G] on the
  * device, any values, NULL: zeros; with causal == 0 prefix must be NULL).  Every query sees itself.
  * q bf16 [T, n_heads, d]; k, v bf16 [T, n_kv_heads, d], n_kv_heads dividing n_heads: query head h reads key head
- * h / (n_heads / n_kv_heads).  slopes: fp32 [n_heads], constants of the model (they get no gradient).  cap: 0, or 1e-6 .. 1e6.
+ * h / (n_heads / n_kv_heads).  slopes: fp32 [n_heads], any finite values, constants of the model (they get no gradient).  cap: 0, or 1e-6 .. 1e6.
  * strides (host, NULL: packed): elements from a row of q, k, v (bwd: and of dq, dk, dv) to the next, 0 for a packed tensor, each
  * a multiple of 8; so q, k and v may be parts of the rows of one projection.  out, dout and lse ([n_heads, T]) are packed.
  * Rows behind the last document (cu_seqlens[G] < n_total) belong to none: their results are left as they were.
@@ -438,7 +438,8 @@ gt_status gt_feature_code_dweights(const float* dtable, const uint32_t* vectors,
  * dk and dv summed over the query heads that share a key head.  dq, dk, dv (bf16) are overwritten; they must not overlap any
  * input.  dq, and where several thread blocks share a key's queries dk and dv (shared key heads, small batches), are accumulated with
  * floating-point atomics in fp32: their low-order bits may differ from run to run.
- * Workspace as for every call (header zero at first).  Forward: 256 bytes and 16 per document and per 256 rows; backward:
+ * Workspace as for every call (header zero at first, and calls that may overlap on the GPU need workspaces of their own: their kernels
+ * count in the header).  Forward: 256 bytes and 16 per document and per 256 rows; backward:
  * (4 d + 32) bytes per row and query head, 8 d per row and key head, and 16 per document and 128 rows.
  * A query with bad arguments returns 0.
  * ------------------------------------------------------------------------------------- */

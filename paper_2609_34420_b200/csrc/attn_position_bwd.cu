@@ -203,7 +203,7 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 
     // Item number k of this CTA; false: there are no more.  give_back: the calling warp is done with its description.
     auto take = [&](int k) -> bool {
-        mbar_wait(bar(kBarItemFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 300);
+        item_wait(bar(kBarItemFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 300);
         return items[k & 1].n > 0 && *abort_flag == 0u;
     };
     auto give_back = [&](int k) {
@@ -218,6 +218,7 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             // The CTA's own number, then what the counter gives, as late as can be: when the last rows of the item before are on their way.
             int32_t index = (int32_t)blockIdx.x;
             int c = 0;                                       // query tiles so far
+            bool good = true;                                // no wait has been given up (then the items are only counted to their end)
             for (int k = 0;; ++k) {
                 Item item{};
                 while (item.n == 0) {
@@ -264,7 +265,7 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         }
                     }
                 }
-                if (k >= 2) mbar_wait(bar(kBarItemEmpty + (k & 1)), ((k >> 1) & 1) ^ 1, abort_flag, p.status, 301);
+                if (k >= 2) good &= item_wait(bar(kBarItemEmpty + (k & 1)), ((k >> 1) & 1) ^ 1, abort_flag, p.status, 301);
                 if (lane == 0) {
                     items[k & 1] = item;
                     mbar_arrive(bar(kBarItemFull + (k & 1)));
@@ -272,21 +273,21 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 __syncwarp();
                 if (item.n == 0) break;
                 const int kv_head = item.head / p.group;
-                if (k >= 2) mbar_wait(bar(kBarKEmpty + (k & 1)), ((k >> 1) & 1) ^ 1, abort_flag, p.status, 302);
-                if (lane == 0) {
+                if (k >= 2) good &= mbar_wait(bar(kBarKEmpty + (k & 1)), ((k >> 1) & 1) ^ 1, abort_flag, p.status, 302);
+                if (good && lane == 0) {
                     mbar_arrive_expect_tx(bar(kBarKFull + (k & 1)), L::kTileBytes);
                     tma_load_3d(smem_u32(smem + L::kK + (k & 1) * L::kTileBytes), &tmap_k, bar(kBarKFull + (k & 1)), 0, kv_head, item.node0 + item.kv0);
                 }
-                if (k >= 1) mbar_wait(bar(kBarVEmpty), (k - 1) & 1, abort_flag, p.status, 303);
-                if (lane == 0) {
+                if (k >= 1) good &= mbar_wait(bar(kBarVEmpty), (k - 1) & 1, abort_flag, p.status, 303);
+                if (good && lane == 0) {
                     mbar_arrive_expect_tx(bar(kBarVFull), L::kTileBytes);
                     tma_load_3d(smem_u32(smem + L::kV), &tmap_v, bar(kBarVFull), 0, kv_head, item.node0 + item.kv0);
                 }
                 const int n_q = item.q_tiles();
                 for (int i = 0; i < n_q; ++i, ++c) {
                     const int s = c & 1;
-                    if (c >= 2) mbar_wait(bar(kBarStageEmpty + s), ((c >> 1) & 1) ^ 1, abort_flag, p.status, 310);
-                    if (lane == 0) {
+                    if (c >= 2) good &= mbar_wait(bar(kBarStageEmpty + s), ((c >> 1) & 1) ^ 1, abort_flag, p.status, 310);
+                    if (good && lane == 0) {
                         const int32_t row = item.node0 + item.q_lo + i * kTile;
                         mbar_arrive_expect_tx(bar(kBarQdoFull + s), 2 * L::kTileBytes + kExtTileBytes);
                         tma_load_3d(smem_u32(smem + L::kQ + s * L::kStageBytes), &tmap_q, bar(kBarQdoFull + s), 0, item.head, row);

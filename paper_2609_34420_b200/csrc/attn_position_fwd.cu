@@ -5,7 +5,7 @@
 // The grid is persistent: a CTA takes one item of work (a head and one or two 128-row query tiles of a document) after the other, and its
 // warps run through them as through one long row of key tiles.  The next item's rows are fetched, and its first scores made, while the
 // last one's outputs are still written; with a CTA per item, 64 causal documents of 512-2 048 tokens spent 40 % of the time on filling and
-// draining (551 -> @@ us).
+// draining (551 -> 460 us).
 //
 //   warp 0      TMA producer: Q (two items' worth) and K, V through 2-stage rings
 //   warp 1      issues S_t = Q_t K^T for both query tiles
@@ -140,7 +140,7 @@ __device__ __forceinline__ void setmaxnreg_dec_56() { asm volatile("setmaxnreg.d
 // kTiles = 1: blocks of one query tile, for grids that would leave half of the SMs idle or more.
 // kCapForm: 0 no cap; 1 a cap of kLeastBoundedCap to kBoundedCap; 2 any cap.  With the second form no score can be out of reach of a reference of half the
 // cap, so that nothing is redone, and P takes the place of the scores chunk by chunk; the registers that this frees are what hides the
-// polynomial's latency (causal 16 384 tokens, cap 30: 665 -> @@ us).
+// polynomial's latency (causal 16 384 tokens, cap 30: 640 -> 530 us).
 // kExact (with the fp32 output): O is divided by the sum of the probabilities as the MMA reads them, rounded to bf16, so that their
 // rounding cancels where a row has few large ones; lse is that of the unrounded ones all the same.  The backward subtracts dout . out from
 // dout . v_j, two nearly equal numbers in such rows: with scores of standard deviation 4, dq was off by 0.6 % (out rounded to bf16 and
@@ -199,7 +199,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 
     // Item number k of this CTA, read by whole warps; false: there are no more.
     auto take = [&](int k, Item& item) -> bool {
-        mbar_wait(bar(kBarItemFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 200);
+        item_wait(bar(kBarItemFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 200);
         item = items[k & 1];
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(kBarItemEmpty + (k & 1)));
@@ -210,10 +210,10 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         if constexpr (kTiles == 2) setmaxnreg_dec_56();
         if (warp == 2) {
             // ---- the items: the CTA's own number, then what the counter gives, as late as its latency allows: the longest items come
-            // first, and who takes the short ones of the end is decided by who is done (two items ahead: causal 16 384 tokens 441 us, now @@) ----
+            // first, and who takes the short ones of the end is decided by who is done (two items ahead: causal 16 384 tokens 441 us, now 370) ----
             int32_t index = (int32_t)blockIdx.x;
             for (int k = 0;; ++k) {
-                if (k > 0) mbar_wait(bar(kBarFetch), (k - 1) & 1, abort_flag, p.status, 203);
+                if (k > 0) item_wait(bar(kBarFetch), (k - 1) & 1, abort_flag, p.status, 203);
                 Item item{};
                 while (item.n == 0) {
                     if (index < 0) {
@@ -259,7 +259,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     if (block >= n_blocks) item.n = 0;
                     else item.prefix = p.prefix ? p.prefix[g] : 0;
                 }
-                if (k >= 2) mbar_wait(bar(kBarItemEmpty + (k & 1)), ((k >> 1) & 1) ^ 1, abort_flag, p.status, 201);
+                if (k >= 2) item_wait(bar(kBarItemEmpty + (k & 1)), ((k >> 1) & 1) ^ 1, abort_flag, p.status, 201);
                 if (lane == 0) {
                     items[k & 1] = item;
                     mbar_arrive(bar(kBarItemFull + (k & 1)));
@@ -271,11 +271,12 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             Item item;
             Span span;
             int c = 0;                                       // key tiles so far
+            bool good = true;                                // no wait has been given up
             for (int k = 0; take(k, item); ++k) {
                 span.set(item, p.causal);
                 const int kv_head = item.head / p.group;
-                if (k >= 2) mbar_wait(bar(kBarQEmpty + (k & 1)), ((k >> 1) & 1) ^ 1, abort_flag, p.status, 210);
-                if (lane == 0) {
+                if (k >= 2) good &= mbar_wait(bar(kBarQEmpty + (k & 1)), ((k >> 1) & 1) ^ 1, abort_flag, p.status, 210);
+                if (good && lane == 0) {
                     mbar_arrive_expect_tx(bar(kBarQFull + (k & 1)), span.tiles * L::kTileBytes);
                     for (int t = 0; t < span.tiles; ++t)
                         tma_load_3d(smem_u32(smem + L::kQ + (2 * (k & 1) + t) * L::kTileBytes), &tmap_q, bar(kBarQFull + (k & 1)), 0, item.head,
@@ -286,13 +287,13 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     if (s == fetch && lane == 0) mbar_arrive(bar(kBarFetch));
                     const int st = c % kStages;
                     const int32_t row = item.node0 + span.key_tile(s) * kTile;
-                    if (c >= kStages) mbar_wait(bar(kBarKEmpty + st), ((c / kStages) & 1) ^ 1, abort_flag, p.status, 211);
-                    if (lane == 0) {
+                    if (c >= kStages) good &= mbar_wait(bar(kBarKEmpty + st), ((c / kStages) & 1) ^ 1, abort_flag, p.status, 211);
+                    if (good && lane == 0) {
                         mbar_arrive_expect_tx(bar(kBarKFull + st), L::kTileBytes);
                         tma_load_3d(smem_u32(smem + L::kK + st * L::kTileBytes), &tmap_k, bar(kBarKFull + st), 0, kv_head, row);
                     }
-                    if (c >= kStages) mbar_wait(bar(kBarVEmpty + st), ((c / kStages) & 1) ^ 1, abort_flag, p.status, 212);
-                    if (lane == 0) {
+                    if (c >= kStages) good &= mbar_wait(bar(kBarVEmpty + st), ((c / kStages) & 1) ^ 1, abort_flag, p.status, 212);
+                    if (good && lane == 0) {
                         mbar_arrive_expect_tx(bar(kBarVFull + st), L::kTileBytes);
                         tma_load_3d(smem_u32(smem + L::kV + st * L::kTileBytes), &tmap_v, bar(kBarVFull + st), 0, kv_head, row);
                     }
@@ -403,7 +404,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         int step0 = 0, own = 0;                 // score tiles, and this query tile's, so far
         for (int k = 0;; ++k) {
         // (the item is read again where its results are written, and given back behind that: fewer registers in between)
-        mbar_wait(bar(kBarItemFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 202);
+        item_wait(bar(kBarItemFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 202);
         if (items[k & 1].n == 0 || *abort_flag != 0u) break;
         Span span;
         span.set(items[k & 1], p.causal);
@@ -420,6 +421,8 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         [[maybe_unused]] float l_rounded = 0.f;
         [[maybe_unused]] bool wide = false;              // a score was out of the polynomial's reach
         [[maybe_unused]] const float slope2 = kSlope ? p.slopes[items[k & 1].head] * kLog2e : 0.f;
+        // (a negative slope favours the farthest key that the row sees: the bound on the scores moves along)
+        if (kBounded && kSlope && slope2 < 0.f) m -= slope2 * (float)max(q, limit - 1 - q);
         [[maybe_unused]] const int32_t prefix = kSlope ? items[k & 1].prefix : 0;
 
         uint32_t sa[kCW], sb[kCW];              // score chunks, alternating

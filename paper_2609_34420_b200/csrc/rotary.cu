@@ -221,7 +221,7 @@ extern "C" gt_status gt_rotary(const void* q, const void* k, const double* frequ
     gt_status st = validate_batch(batch);
     if (st != GT_OK) return st;
     if (n_heads < 1 || n_kv_heads < 0 || !q || !q_out || !frequencies || (n_kv_heads > 0 && (!k || !k_out))) return GT_ERR_INVALID_ARG;
-    if (rot_dim < 2 || rot_dim % 2 != 0 || rot_dim > head_dim) return GT_ERR_INVALID_ARG;
+    if (rot_dim < 2 || rot_dim % 2 != 0 || rot_dim > head_dim || reinterpret_cast<uintptr_t>(frequencies) % 8 != 0) return GT_ERR_INVALID_ARG;
     if (dtype != GT_BF16 && dtype != GT_FP16 && dtype != GT_FP32) return GT_ERR_INVALID_ARG;
     if (head_dim != 32 && head_dim != 64) return GT_ERR_UNSUPPORTED;
     if (n_heads > 65535 || n_kv_heads > 65535) return GT_ERR_UNSUPPORTED;

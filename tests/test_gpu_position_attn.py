@@ -363,3 +363,9 @@ def test_counters_are_zero_between_calls():
     for ws in (c.forward(), c.backward()):
         torch.cuda.synchronize()
         assert not ws[:256].any()
+
+
+@pytest.mark.parametrize("options", [dict(), dict(cap=30.0, spread=4.0), dict(causal=False), dict(causal=False, cap=10.0), dict(prefix=[200], cap=50.0)])
+def test_slopes_of_either_sign(options):
+    """A negative slope is a bonus on distance: the largest scores are the farthest keys'."""
+    Case([500], H=4, G=4, slopes=[-0.5, 0.5, -3.0, 0.0], seed=27, **options).run()

@@ -175,7 +175,7 @@ def rotary(b=None, q=A, k=A, f=A, p=None, H=4, G=2, d=64, rot=64, dtype=0, sq=0,
                                        (dict(H=0), 1), (dict(G=-1), 1), (dict(rot=0), 1), (dict(rot=3), 1), (dict(rot=66), 1), (dict(d=48, rot=32), 2),
                                        (dict(d=128), 2), (dict(dtype=3), 1), (dict(dtype=-1), 1), (dict(sq=255), 1), (dict(sk=-8), 1), (dict(tq=1), 1),
                                        (dict(tk=1 << 40), 1), (dict(q=A + 1), 1), (dict(dtype=2, ok=(1 << 25) + 2), 1), (dict(oq=A, sq=512), 1),
-                                       (dict(H=65536), 2)])
+                                       (dict(H=65536), 2), (dict(f=A + 4), 1)])
 def test_rotary_refuses(kw, status):
     assert rotary(**kw) == status
 
