@@ -2,12 +2,15 @@
 
     python -m paper_2609_34420_b200.profile_case WORKLOAD [REPS] [spd|fwd|bwd|chunked|all]
     python -m paper_2609_34420_b200.profile_case featN [REPS] [VECTORS]
+    python -m paper_2609_34420_b200.profile_case seqN [REPS] [CAP]
 
 WORKLOAD is one of the named workloads (tiny_er256, ba4096, powerlaw16k, powerlaw64k,
 varlen_rgg64) or plN for a power-law graph of N nodes (H=8, d=64, max_dist=24).  A small,
 self-contained timing command line for one entry point at a time.  featN times the feature-bias
 variant on N nodes (H=8, d=64) with VECTORS distinct feature vectors (default 12): the path for any
-features, and the code matrix through the tensor-core kernels of the bucket form.
+features, and the code matrix through the tensor-core kernels of the bucket form.  seqN times a layer
+on a causal document of N tokens (H=8, d=64): rotary positions, attention forward (with the fp32 output that
+its backward takes) and backward, with scores capped at CAP if given.
 """
 from __future__ import annotations
 
@@ -88,11 +91,43 @@ def feature_case(n: int, reps: int, n_vec: int) -> int:
     return 0
 
 
+def sequence_timings(n: int, reps: int, cap: float) -> dict:
+    """CUDA-event timings (ms) of rotary positions and attention on a causal document of n tokens, H=8, d=64."""
+    H, d = 8, 64
+    dev = torch.device("cuda", torch.cuda.current_device())
+    g = torch.Generator(device=dev).manual_seed(1)
+    q, k, v, do = (torch.randn(n, H, d, device=dev, generator=g).bfloat16() for _ in range(4))
+    qr, kr, out, dq, dk, dv = (torch.empty_like(q) for _ in range(6))
+    out32, lse = torch.empty(n, H, d, device=dev), torch.empty(H, n, device=dev)
+    batch, f = gt.Batch(n), gt.gt_rotary_frequencies(d).to(dev)
+    pairs = n * (n + 1) // 2
+    res = {"rotary_bytes": 8.0 * n * H * d, "fwd_flops": 4.0 * H * d * pairs, "bwd_flops": 10.0 * H * d * pairs}
+    res["rotary_ms"] = timed_ms(lambda: gt.gt_rotary(q, k, f, None, batch, False, 1.0, False, qr, kr), reps)
+    ws_f = gt.gt_position_attn_fwd(qr, kr, v, None, None, batch, True, cap, out, lse, out32)
+    res["fwd_ms"] = timed_ms(lambda: gt.gt_position_attn_fwd(qr, kr, v, None, None, batch, True, cap, out, lse, None, ws_f), reps)
+    res["fwd_f32_ms"] = timed_ms(lambda: gt.gt_position_attn_fwd(qr, kr, v, None, None, batch, True, cap, out, lse, out32, ws_f), reps)
+    ws_b = gt.gt_position_attn_bwd(qr, kr, v, out, do, lse, None, None, batch, True, cap, dq, dk, dv, out32)
+    res["bwd_ms"] = timed_ms(lambda: gt.gt_position_attn_bwd(qr, kr, v, out, do, lse, None, None, batch, True, cap, dq, dk, dv, out32, ws_b), reps)
+    gt.gt_check(ws_f)
+    gt.gt_check(ws_b)
+    return res
+
+
+def sequence_case(n: int, reps: int, cap: float) -> int:
+    r = sequence_timings(n, reps, cap)
+    print(f"rotary {r['rotary_ms']:.4f} ms  {r['rotary_bytes'] / r['rotary_ms'] / 1e6:.1f} GB/s")
+    for name, flops in (("fwd", "fwd_flops"), ("fwd_f32", "fwd_flops"), ("bwd", "bwd_flops")):
+        print(f"position attention {name} {r[name + '_ms']:.3f} ms  {r[flops] / r[name + '_ms'] / 1e9:.1f} TFLOP/s")
+    return 0
+
+
 def main(argv) -> int:
     name = argv[1] if len(argv) > 1 else "powerlaw16k"
     reps = int(argv[2]) if len(argv) > 2 else 1
     if name.startswith("feat") and name[4:].isdigit():
         return feature_case(int(name[4:]), reps, int(argv[3]) if len(argv) > 3 else 12)
+    if name.startswith("seq") and name[3:].isdigit():
+        return sequence_case(int(name[3:]), reps, float(argv[3]) if len(argv) > 3 else 0.0)
     what = argv[3] if len(argv) > 3 else "all"
     if name.startswith("pl") and name[2:].isdigit():
         w = wl.Workload(name, wl.pack_graphs([wl.chung_lu_power_law(int(name[2:]), 12.0, 2.1, 0)]), 8, 64, 24)
