@@ -491,7 +491,9 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         for (int i = 0; i < n_q; ++i, ++c) {
             const int32_t q0 = q_lo + i * kTile + grp * 32;                     // the group's first query
             const bool masked = q0 < last_from || q0 + 32 > n || key0 + 32 > n;     // some pair of the warp's may not count
-            const int c_from = from - q0, c_to = to - q0;
+            // bit e: this thread's key is seen by the group's query e
+            const uint32_t seen = (to - q0 >= 32 ? 0xffffffffu : to > q0 ? (1u << (to - q0)) - 1u : 0u) &
+                                  (from - q0 >= 32 ? 0u : from > q0 ? 0xffffffffu << (from - q0) : 0xffffffffu);
             // Penalty on distance: linear in the column where all queries lie behind the keys (or masked ones before them do not matter) or
             // all before; else made for every element.
             const bool behind = q0 >= key0 + 31 || (p.causal && key0 >= prefix), before = q0 + 31 <= key0;
@@ -556,8 +558,8 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         lo = ex2_approx(lo);
                         hi = ex2_approx(hi);
                         if constexpr (decltype(masked_)::value) {
-                            if (e < c_from || e >= c_to) lo = 0.f;
-                            if (e + 1 < c_from || e + 1 >= c_to) hi = 0.f;
+                            if (!(seen & (1u << e))) lo = 0.f;
+                            if (!(seen & (2u << e))) hi = 0.f;
                         }
                         pk[e >> 1] = pack_bf16x2(lo, hi);
                         if constexpr (kCap) {
@@ -596,20 +598,19 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             tmem_wait_ld();
 
             // ---------------- dS^T = P^T o (dP^T - Delta) ----------------
-            auto ds_round = [&](int rnd, const uint32_t (&dp)[16], auto masked_) {
+            auto ds_round = [&](int rnd, const uint32_t (&dp)[16], auto foreign) {
 #pragma unroll
                 for (int k = 0; k < 16; k += 2) {
                     const int e = rnd * 16 + k;
                     float lo, hi;
                     unpack_f32x2(mul_f32x2(pack_f32x2(pr[e], pr[e + 1]), pack_u32x2(dp[k], dp[k + 1])), lo, hi);
-                    if constexpr (decltype(masked_)::value) {      // (0 x NaN: a row of V that is another document's, or of this one's queries that do not see the key)
-                        if (e < c_from || e >= c_to) lo = 0.f;
-                        if (e + 1 < c_from || e + 1 >= c_to) hi = 0.f;
+                    if constexpr (decltype(foreign)::value) {      // (0 x NaN: dP of a row of V that is another document's)
+                        if (key >= n) lo = hi = 0.f;
                     }
                     pk[e >> 1] = pack_bf16x2(lo, hi);
                 }
             };
-            if (masked) {
+            if (key0 + 32 > n) {
                 ds_round(0, dpa, Tag<true>{});
                 ds_round(1, dpb, Tag<true>{});
             } else {
