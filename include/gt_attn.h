@@ -431,7 +431,7 @@ gt_status gt_feature_code_dweights(const float* dtable, const uint32_t* vectors,
  *
  * out_f32: fp32 [T, n_heads, d], or NULL: the output before its rounding, for the backward.  Where a row has few large
  * probabilities, dout . out is subtracted from nearly equal numbers, and the rounding of a bf16 out alone moves dq and dk by half a
- * per cent (scores of standard deviation 4; 0.3 % with out_f32); the forward also forms it with more care (and 2 to 10 % slower).
+ * per cent (scores of standard deviation 4; 0.3 % with out_f32); the forward also forms it with more care (and takes 10 to 30 % longer).
  * The backward takes out (which may be NULL beside an out_f32), out_f32 and lse of the forward with the same arguments.  With P = exp(S - lse), Delta_i = dout_i . out_i:
  *     dv_j = sum P_ij dout_i,   dS_ij = P_ij (dout_i . v_j - Delta_i) (1 - tanh^2(x_ij / cap)),
  *     dq_i = sum_j dS_ij k_j / sqrt(d),   dk_j = sum dS_ij q_i / sqrt(d),

@@ -9,7 +9,7 @@
 //
 //   warp 0      TMA producer: Q (two items' worth) and K, V through 2-stage rings
 //   warp 1      issues S_t = Q_t K^T for both query tiles
-//   warp 2      fetches the items, two ahead
+//   warp 2      fetches the items
 //   warp 3      issues O_t += P_t V (A from TMEM, B = V as MN-major); clears what lies behind the document in its last V tile
 //   warps 4-19  softmax: 8 warps per query tile, 4 per half of the 128 key columns (thread = query row = TMEM lane, 64 scores)
 //
@@ -137,10 +137,11 @@ constexpr int kNbPair = 2;                    // named barriers: + 4 t + lane qu
 // register budget with two tiles: the CTA is launched with 640 x 96 registers and shares out 128 x 56 + 512 x 104 = 60416 <= 61440
 __device__ __forceinline__ void setmaxnreg_dec_56() { asm volatile("setmaxnreg.dec.sync.aligned.u32 56;"); }
 
-// kTiles = 1: blocks of one query tile, for grids that would leave half of the SMs idle or more.
+// kTiles = 1: items of one query tile, for grids that end sooner with them (one_tile_blocks).
 // kCapForm: 0 no cap; 1 a cap of kLeastBoundedCap to kBoundedCap; 2 any cap.  With the second form no score can be out of reach of a reference of half the
 // cap, so that nothing is redone, and P takes the place of the scores chunk by chunk; the registers that this frees are what hides the
-// polynomial's latency (causal 16 384 tokens, cap 30: 640 -> 530 us).
+// polynomial's latency (causal 16 384 tokens, cap 30: 640 -> 530 us; with coefficients
+// made for the scores themselves, and whole sectors per store, 490).
 // kExact (with the fp32 output): O is divided by the sum of the probabilities as the MMA reads them, rounded to bf16, so that their
 // rounding cancels where a row has few large ones; lse is that of the unrounded ones all the same.  The backward subtracts dout . out from
 // dout . v_j, two nearly equal numbers in such rows: with scores of standard deviation 4, dq was off by 0.6 % (out rounded to bf16 and
