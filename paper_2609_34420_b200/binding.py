@@ -530,17 +530,20 @@ def gt_feature_code_dweights(dtable, vectors, dweights) -> None:
            "gt_feature_code_dweights")
 
 
-def _rows(t: Optional[torch.Tensor]):
+def _rows(t: Optional[torch.Tensor], n_total: int, heads: int, d: int):
     """Address and row stride (0: packed) of a [T, heads, d] tensor whose rows are contiguous, but may lie apart (parts of a projection)."""
     if t is None:
         return None, 0
     if not t.is_cuda:
         raise ValueError("expected a CUDA tensor")
+    rows, *row = t.shape
+    if rows < n_total or row != [heads, d]:
+        raise ValueError(f"expected a tensor [{n_total}, {heads}, {d}]")
     if t.is_contiguous():
         return t.data_ptr(), 0
-    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
-        raise ValueError("expected a tensor [T, heads, d] with contiguous rows")
-    return t.data_ptr(), t.stride(0)
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d) or (t.stride(0) < heads * d and n_total > 1):
+        raise ValueError("expected a tensor [T, heads, d] with contiguous rows that do not overlap")
+    return t.data_ptr(), t.stride(0) if n_total > 1 else 0
 
 
 def _same_dtype(dtype, *tensors) -> None:
@@ -549,14 +552,20 @@ def _same_dtype(dtype, *tensors) -> None:
             raise ValueError(f"expected tensors of type {dtype}")
 
 
+def _holds(n: int, *tensors) -> None:
+    for t in tensors:
+        if t is not None and t.numel() < n:
+            raise ValueError(f"expected a tensor of {n} elements")
+
+
 def gt_position_attn_fwd_workspace(batch: Batch, n_heads: int, n_kv_heads: int, head_dim: int) -> int:
     b = batch._c_pair()[1]
     return int(lib().gt_position_attn_fwd_workspace(b, n_heads, n_kv_heads, head_dim))
 
 
-def _position_strides(*tensors):
+def _position_strides(n_total: int, H: int, G: int, d: int, *tensors):
     """Reference to the C struct of the row strides of q, k, v(, dq, dk, dv), None where all are packed, and the addresses."""
-    pointers, strides = zip(*[_rows(t) for t in tensors])
+    pointers, strides = zip(*[_rows(t, n_total, G if i % 3 else H, d) for i, t in enumerate(tensors)])
     return (ctypes.byref(_GtRowStrides(*strides)) if any(strides) else None), pointers
 
 
@@ -570,9 +579,14 @@ def gt_position_attn_fwd(q, k, v, slopes: Optional[torch.Tensor], prefix: Option
     _same_dtype(torch.bfloat16, q, k, v, out)
     _same_dtype(torch.float32, slopes, lse, out_f32)
     _same_dtype(torch.int32, prefix)
+    T = batch.n_total
+    strides, (pq, pk, pv) = _position_strides(T, H, G, d, q, k, v)
+    _holds(T * H * d, out, out_f32)
+    _holds(T * H, lse)
+    _holds(H, slopes)
+    _holds(batch.n_graphs, prefix)
     if workspace is None:
         workspace = _workspace(gt_position_attn_fwd_workspace(batch, H, G, d), q.device)
-    strides, (pq, pk, pv) = _position_strides(q, k, v)
     st = lib().gt_position_attn_fwd(pq, pk, pv, _ptr(slopes), _ptr(prefix), batch._c_pair()[1], H, G, d, strides,
                                     int(causal), float(cap), _ptr(out), _ptr(lse), _ptr(out_f32), _ptr(workspace), workspace.numel(), _stream())
     _raise(st, "gt_position_attn_fwd")
@@ -593,9 +607,14 @@ def gt_position_attn_bwd(q, k, v, out, dout, lse, slopes: Optional[torch.Tensor]
     _same_dtype(torch.bfloat16, q, k, v, out, dout, dq, dk, dv)
     _same_dtype(torch.float32, slopes, lse, out_f32)
     _same_dtype(torch.int32, prefix)
+    T = batch.n_total
+    strides, (pq, pk, pv, pdq, pdk, pdv) = _position_strides(T, H, G, d, q, k, v, dq, dk, dv)
+    _holds(T * H * d, out, out_f32, dout)
+    _holds(T * H, lse)
+    _holds(H, slopes)
+    _holds(batch.n_graphs, prefix)
     if workspace is None:
         workspace = _workspace(gt_position_attn_bwd_workspace(batch, H, G, d), q.device)
-    strides, (pq, pk, pv, pdq, pdk, pdv) = _position_strides(q, k, v, dq, dk, dv)
     st = lib().gt_position_attn_bwd(pq, pk, pv, _ptr(out), _ptr(out_f32), _ptr(dout), _ptr(lse), _ptr(slopes), _ptr(prefix), batch._c_pair()[1],
                                     H, G, d, strides, int(causal), float(cap), pdq, pdk, pdv,
                                     _ptr(workspace), workspace.numel(), _stream())
@@ -614,8 +633,10 @@ def gt_rotary(q, k: Optional[torch.Tensor], frequencies, positions: Optional[tor
         raise ValueError("expected bf16, fp16 or fp32")
     if (k is None) != (k_out is None):
         raise ValueError("expected k and k_out, or neither")
-    (pq, sq), (pk, sk), (oq, tq), (ok, tk) = (_rows(t) for t in (q, k, q_out, k_out))
-    st = lib().gt_rotary(pq, pk, _ptr(frequencies), _ptr(positions), batch._c_pair()[1], H, 0 if k is None else k.shape[1], d,
+    T, G = batch.n_total, 0 if k is None else k.shape[1]
+    (pq, sq), (pk, sk), (oq, tq), (ok, tk) = (_rows(t, T, G if i % 2 else H, d) for i, t in enumerate((q, k, q_out, k_out)))
+    _holds(T, positions)
+    st = lib().gt_rotary(pq, pk, _ptr(frequencies), _ptr(positions), batch._c_pair()[1], H, G, d,
                          2 * frequencies.numel(), DTYPES[q.dtype], int(interleaved), float(scale), int(inverse), sq, sk, tq, tk,
                          oq, ok, _stream())
     _raise(st, "gt_rotary")

@@ -192,3 +192,49 @@ def test_bindings_refuse_what_the_library_cannot_see():
         gt.gt_rotary(q.double(), None, torch.ones(32, dtype=torch.float64), None, gt.Batch(4), False, 1.0, False, q.double(), None)
     with pytest.raises(ValueError):
         gt.gt_position_attn_fwd(q, q, q, None, None, gt.Batch(4), True, 0.0, q, torch.zeros(2, 4))
+
+
+class _OnGpu:
+    """A tensor that passes for one on the GPU: a refused call does not look at its memory."""
+    is_cuda = True
+
+    def __init__(self, t):
+        self.t = t
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+
+def _bf16(*shape):
+    return _OnGpu(torch.zeros(shape, dtype=torch.bfloat16))
+
+
+@pytest.mark.parametrize("name,wrong", [
+    ("k", lambda: _OnGpu(torch.zeros(1, 2, 64, dtype=torch.bfloat16).expand(8, 2, 64))),       # one row for all: would be taken for packed rows
+    ("q", lambda: _OnGpu(torch.zeros(8, 1, 64, dtype=torch.bfloat16).expand(8, 4, 64))),
+    ("q", lambda: _OnGpu(torch.zeros(2000, dtype=torch.bfloat16).as_strided((8, 4, 64), (192, 64, 1)))),
+    ("q", lambda: _bf16(7, 4, 64)), ("k", lambda: _bf16(7, 2, 64)), ("v", lambda: _bf16(8, 1, 64)), ("v", lambda: _bf16(8, 2, 32)), ("out", lambda: _bf16(8, 2, 64)),
+    ("lse", lambda: _OnGpu(torch.zeros(4, 7))), ("slopes", lambda: _OnGpu(torch.zeros(2))), ("prefix", lambda: _OnGpu(torch.zeros(0, dtype=torch.int32))),
+    ("dq", lambda: _bf16(8, 2, 64)), ("dk", lambda: _bf16(8, 4, 64)), ("dv", lambda: _bf16(4, 2, 64)), ("dout", lambda: _bf16(8, 4, 32)),
+    ("out_f32", lambda: _OnGpu(torch.zeros(8, 4, 32)))])
+def test_bindings_refuse_tensors_that_are_too_small(name, wrong):
+    a = dict(q=_bf16(8, 4, 64), k=_bf16(8, 2, 64), v=_bf16(8, 2, 64), out=_bf16(8, 4, 64), dout=_bf16(8, 4, 64), lse=_OnGpu(torch.zeros(4, 8)),
+             slopes=None, prefix=None, batch=gt.Batch(8), causal=True, cap=0.0, dq=_bf16(8, 4, 64), dk=_bf16(8, 2, 64), dv=_bf16(8, 2, 64), out_f32=None,
+             workspace=_OnGpu(torch.zeros(256, dtype=torch.uint8)))
+    a[name] = wrong()
+    with pytest.raises(ValueError):
+        gt.gt_position_attn_bwd(**a)
+    if name not in ("dout", "dq", "dk", "dv"):
+        with pytest.raises(ValueError):
+            gt.gt_position_attn_fwd(**{x: a[x] for x in a if x not in ("dout", "dq", "dk", "dv")})
+
+
+@pytest.mark.parametrize("name,wrong", [("q", lambda: _bf16(7, 4, 64)), ("k", lambda: _OnGpu(torch.zeros(1, 2, 64, dtype=torch.bfloat16).expand(8, 2, 64))),
+                                        ("q_out", lambda: _bf16(8, 2, 64)), ("k_out", lambda: _bf16(8, 1, 64)),
+                                        ("positions", lambda: _OnGpu(torch.zeros(7, dtype=torch.int32)))])
+def test_rotary_binding_refuses_tensors_that_are_too_small(name, wrong):
+    a = dict(q=_bf16(8, 4, 64), k=_bf16(8, 2, 64), frequencies=_OnGpu(torch.ones(32, dtype=torch.float64)), positions=None, batch=gt.Batch(8),
+             interleaved=False, scale=1.0, inverse=False, q_out=_bf16(8, 4, 64), k_out=_bf16(8, 2, 64))
+    a[name] = wrong()
+    with pytest.raises(ValueError):
+        gt.gt_rotary(**a)
