@@ -5,8 +5,8 @@
 // Bound by memory: every row is read and written once.  A block has some consecutive tokens: it makes the cosines and sines of their
 // pairs once for all heads, into shared memory, while its first rows are on their way, and then rotates 32 bytes of a head at a time.
 //
-// The angle is reduced in fp64: turns = position * frequency / 2 pi, less the next whole number, is off by 2^-52 of itself, 5e-7 rad at
-// position 2^31; in fp32 a position of a million would leave nothing of it.  What is left goes to sincospi in fp32.
+// The angle is reduced in fp64: turns = position * frequency / 2 pi, less the next whole number, is off by at most 3 x 2^-53 of itself (three
+// roundings), 7e-7 rad at position 2^31; in fp32 a position of a million would leave nothing of it.  What is left goes to sincospi in fp32.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -267,13 +267,14 @@ extern "C" gt_status gt_rotary_frequencies(int32_t rot_dim, double base, gt_rota
                                            double original_length, double low, double high, double* frequencies_host)
 {
     if (!frequencies_host || rot_dim < 2 || rot_dim % 2 != 0 || !(base > 0.0) || !isfinite(base)) return GT_ERR_INVALID_ARG;
-    if (scaling != GT_ROTARY_PLAIN && (!(factor > 0.0) || !isfinite(factor))) return GT_ERR_INVALID_ARG;
+    if (scaling != GT_ROTARY_PLAIN && (!(factor > 0.0) || !isfinite(factor) || !isfinite(1.0 / factor))) return GT_ERR_INVALID_ARG;
     switch (scaling) {
         case GT_ROTARY_PLAIN: factor = 1.0; break;
         case GT_ROTARY_LINEAR: break;
         case GT_ROTARY_BASE:
             if (rot_dim == 2) return GT_ERR_INVALID_ARG;
             base *= pow(factor, (double)rot_dim / (rot_dim - 2));
+            if (!(base > 0.0) || !isfinite(base)) return GT_ERR_INVALID_ARG;
             factor = 1.0;
             break;
         case GT_ROTARY_PARTS:

@@ -238,3 +238,10 @@ def test_rotary_binding_refuses_tensors_that_are_too_small(name, wrong):
     a[name] = wrong()
     with pytest.raises(ValueError):
         gt.gt_rotary(**a)
+
+
+@pytest.mark.parametrize("args", [(8, 1e300, "base", 1e10), (4, 1e4, "base", 1e-200), (8, 1e4, "linear", 1e-310), (8, 1e4, "parts", 1e-310, 4096, 1.0, 4.0)])
+def test_frequencies_refuse_what_leaves_the_range(args):
+    with pytest.raises(gt.GtError) as e:
+        gt.gt_rotary_frequencies(*args)
+    assert e.value.status == 1
