@@ -422,7 +422,8 @@ gt_status gt_feature_code_dweights(const float* dtable, const uint32_t* vectors,
  * over the keys j that i sees: all of its document (causal == 0), or j <= i and j < prefix[g] (causal != 0; prefix int32[G] on the
  * device, any values, NULL: zeros; with causal == 0 prefix must be NULL).  Every query sees itself.
  * q bf16 [T, n_heads, d]; k, v bf16 [T, n_kv_heads, d], n_kv_heads dividing n_heads: query head h reads key head
- * h / (n_heads / n_kv_heads).  slopes: fp32 [n_heads], any finite values, constants of the model (they get no gradient).  cap: 0, or 1e-6 .. 1e6.
+ * h / (n_heads / n_kv_heads).  slopes: fp32 [n_heads], constants of the model (they get no
+ * gradient), of either sign, slope x the longest document from -1e6 to 1e30 (scores are formed in fp32, which resolves 2^-24 of their size).  cap: 0, or 1e-6 .. 1e6.
  * strides (host, NULL: packed): elements from a row of q, k, v (bwd: and of dq, dk, dv) to the next, 0 for a packed tensor, each
  * a multiple of 8; so q, k and v may be parts of the rows of one projection.  out, dout and lse ([n_heads, T]) are packed.
  * Rows behind the last document (cu_seqlens[G] < n_total) belong to none: their results are left as they were.
@@ -470,7 +471,7 @@ gt_status gt_position_attn_bwd(const void* q, const void* k, const void* v, cons
  * *_stride elements apart (0: packed); q_out, k_out likewise.  An output may be its input (same address, same stride); otherwise
  * outputs must not overlap inputs.  positions: int32 [T] on the device, any values, or NULL: a row's index in its document.
  * frequencies: fp64 [rot_dim / 2] on the device, radians per position; rot_dim even, 2 .. head_dim; head_dim 32 or 64.
- * Angles are reduced in fp64 (within 5e-7 rad at 2^31 positions x 1 rad), results rounded once.  Rows behind the last document
+ * Angles are reduced in fp64 (within 1e-6 rad at 2^31 positions x 1 rad), results rounded once.  Rows behind the last document
  * are left as they were.  Rows at 16-byte addresses and strides, and with the halves 2 * 16 bytes' worth of rot_dim, are fastest;
  * any other element's address is taken, too.  No workspace.
  *

@@ -95,6 +95,10 @@ __device__ __forceinline__ float tanh_any(float y)
     return u <= kTanhReach ? p : fmaf(-2.0f, r, 1.0f);
 }
 
+// A penalty that is carried from column to column loses 2^-24 of the largest one on the way at each step; on the score of a query's own key, which has
+// none, that leaves up to 2^-20 of a slope (backward 2^-16).  Slopes above this (in log2 units; usual ones are below 1) are multiplied out there.
+constexpr float kSteep = 64.0f;
+
 // Words of the workspace's header that no other call uses: counters of the persistent kernels, 0 between calls.
 constexpr int kNextForward = 16, kNextBackward = 17;
 

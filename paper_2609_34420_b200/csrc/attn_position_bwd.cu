@@ -478,6 +478,8 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         const int32_t from = p.causal && key >= prefix ? key : 0, to = key < n ? n : 0;
         const int32_t last_from = p.causal && key0 + 31 >= prefix ? key0 + 31 : 0;               // largest `from` of the warp
         [[maybe_unused]] const float slope2 = kSlope ? p.slopes[items[k & 1].head] * kLog2e : 0.f;
+        // (steep penalties: made for every element wherever a key's own query is, see kSteep)
+        [[maybe_unused]] const bool linear = p.causal && key0 >= prefix && fabsf(slope2) <= kSteep;
         // lse of the warp's queries, a lane each, fetched a tile ahead
         [[maybe_unused]] const float* lse_row = p.lse + (size_t)items[k & 1].head * p.n_total + items[k & 1].node0;
         [[maybe_unused]] auto fetch_lse = [&](int i) -> float {
@@ -496,7 +498,7 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                                   (from - q0 >= 32 ? 0u : from > q0 ? 0xffffffffu << (from - q0) : 0xffffffffu);
             // Penalty on distance: linear in the column where all queries lie behind the keys (or masked ones before them do not matter) or
             // all before; else made for every element.
-            const bool behind = q0 >= key0 + 31 || (p.causal && key0 >= prefix), before = q0 + 31 <= key0;
+            const bool behind = q0 >= key0 + 31 || linear, before = q0 + 31 <= key0;
             [[maybe_unused]] const bool mixed = kSlope && !before && !behind;
             [[maybe_unused]] const float step_slope = behind ? -slope2 : slope2;
             if constexpr (kCap) {

@@ -424,7 +424,8 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         [[maybe_unused]] const float slope2 = kSlope ? p.slopes[items[k & 1].head] * kLog2e : 0.f;
         // (a negative slope favours the farthest key that the row sees: the bound on the scores moves along)
         if (kBounded && kSlope && slope2 < 0.f) m -= slope2 * (float)max(q, limit - 1 - q);
-        [[maybe_unused]] const int32_t prefix = kSlope ? items[k & 1].prefix : 0;
+        // (steep penalties: made for every element wherever a row's own key is, see kSteep)
+        [[maybe_unused]] const int32_t linear_from = kSlope ? fabsf(slope2) > kSteep ? INT32_MAX : items[k & 1].prefix : 0;
 
         uint32_t sa[kCW], sb[kCW];              // score chunks, alternating
         uint32_t tS = 0;                        // this thread's score columns of the current step
@@ -447,7 +448,7 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             // Penalty on distance.  Where no key lies behind the query (or, for masked ones, it does not matter) it is linear in the
             // column: (key - query) slope.  Otherwise keys behind all of the warp's rows have it the other way round, and in between
             // a distance is made for every element.
-            const bool before = kv0 + kCols - 1 <= row0 || (p.causal && kv0 >= prefix), behind = kv0 >= row0 + 31;
+            const bool before = kv0 + kCols - 1 <= row0 || (p.causal && kv0 >= linear_from), behind = kv0 >= row0 + 31;
             [[maybe_unused]] const bool mixed = kSlope && !before && !behind;
             [[maybe_unused]] const float step_slope = before ? slope2 : -slope2, ahead = (float)(kv0 - q);       // ahead: the first key's distance
             [[maybe_unused]] uint32_t pk[32];      // P of this thread's columns, bf16 pairs

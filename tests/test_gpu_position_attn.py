@@ -369,3 +369,23 @@ def test_counters_are_zero_between_calls():
 def test_slopes_of_either_sign(options):
     """A negative slope is a bonus on distance: the largest scores are the farthest keys'."""
     Case([500], H=4, G=4, slopes=[-0.5, 0.5, -3.0, 0.0], seed=27, **options).run()
+
+
+@pytest.mark.parametrize("options", [dict(), dict(causal=False), dict(cap=30.0), dict(causal=False, cap=1000.0)])
+def test_slopes_that_leave_a_query_itself_only(options):
+    """Penalties far beyond the range of the exponentials, up to the largest documented: every query's output is its own value."""
+    c = Case([300, 150], H=4, G=4, slopes=[1e3, 1e9, 1e20, 1e27], seed=28, **options)
+    gt.gt_check(c.forward())
+    gt.gt_check(c.backward())
+    ref = c.check(names=("out", "lse", "dv"))
+    assert torch.equal(c.out, c.v)
+    # dq and dk are 0: what is left of dP - Delta, two sums of the same products in fp32, has the elementwise bound only (a norm that counts
+    # roundings of the results to bf16 is 0, too)
+    got = c.results()
+    for name in ("dq", "dk"):
+        assert np.all(np.abs(got[name] - ref[name]) <= ref["bounds"][name]), name
+
+
+def test_one_row_of_a_projection():
+    """A single token's tensors count as packed, whatever stride their only row has."""
+    Case([1], H=4, G=2, seed=29, apart=True).run()
