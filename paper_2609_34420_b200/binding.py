@@ -530,32 +530,32 @@ def gt_feature_code_dweights(dtable, vectors, dweights) -> None:
            "gt_feature_code_dweights")
 
 
-def _rows(t: Optional[torch.Tensor], n_total: int, heads: int, d: int):
-    """Address and row stride (0: packed) of a [T, heads, d] tensor whose rows are contiguous, but may lie apart (parts of a projection)."""
+def _dense(t: Optional[torch.Tensor], dtype, n: int) -> Optional[int]:
+    """Address of a packed tensor of at least n elements."""
     if t is None:
-        return None, 0
-    if not t.is_cuda:
-        raise ValueError("expected a CUDA tensor")
-    rows, *row = t.shape
-    if rows < n_total or row != [heads, d]:
-        raise ValueError(f"expected a tensor [{n_total}, {heads}, {d}]")
+        return None
+    if not t.is_cuda or t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous CUDA tensor of {n} elements of type {dtype}")
+    return t.data_ptr()
+
+
+def _rows(t: torch.Tensor, dtype, shape) -> tuple:
+    """Address and row stride (0: packed) of a [T, heads, d] tensor whose rows are contiguous, but may lie apart (parts of a projection)."""
+    if not t.is_cuda or t.dtype is not dtype:
+        raise ValueError(f"expected a CUDA tensor of type {dtype}")
+    n_total, heads, d = shape
+    if t.shape != shape and (t.dim() != 3 or t.shape[0] < n_total or t.shape[1:] != shape[1:]):
+        raise ValueError(f"expected a tensor {list(shape)}")
     if t.is_contiguous():
         return t.data_ptr(), 0
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d) or (t.stride(0) < heads * d and n_total > 1):
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d) or (n_total > 1 and t.stride(0) < heads * d):
         raise ValueError("expected a tensor [T, heads, d] with contiguous rows that do not overlap")
     return t.data_ptr(), t.stride(0) if n_total > 1 else 0
 
 
-def _same_dtype(dtype, *tensors) -> None:
-    for t in tensors:
-        if t is not None and t.dtype is not dtype:
-            raise ValueError(f"expected tensors of type {dtype}")
-
-
-def _holds(n: int, *tensors) -> None:
-    for t in tensors:
-        if t is not None and t.numel() < n:
-            raise ValueError(f"expected a tensor of {n} elements")
+def _strides(*strides):
+    """Reference to the C struct of the row strides of q, k, v(, dq, dk, dv); None where all are packed."""
+    return ctypes.byref(_GtRowStrides(*strides)) if any(strides) else None
 
 
 def gt_position_attn_fwd_workspace(batch: Batch, n_heads: int, n_kv_heads: int, head_dim: int) -> int:
@@ -563,32 +563,20 @@ def gt_position_attn_fwd_workspace(batch: Batch, n_heads: int, n_kv_heads: int, 
     return int(lib().gt_position_attn_fwd_workspace(b, n_heads, n_kv_heads, head_dim))
 
 
-def _position_strides(n_total: int, H: int, G: int, d: int, *tensors):
-    """Reference to the C struct of the row strides of q, k, v(, dq, dk, dv), None where all are packed, and the addresses."""
-    pointers, strides = zip(*[_rows(t, n_total, G if i % 3 else H, d) for i, t in enumerate(tensors)])
-    return (ctypes.byref(_GtRowStrides(*strides)) if any(strides) else None), pointers
-
-
 def gt_position_attn_fwd(q, k, v, slopes: Optional[torch.Tensor], prefix: Optional[torch.Tensor], batch: Batch,
                          causal: bool, cap: float, out, lse, out_f32: Optional[torch.Tensor] = None,
                          workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention over token sequences: q [T, H, d], k and v [T, G, d] (rows may lie apart), slopes fp32 [H], prefix int32 [documents];
     ``out_f32``, fp32 [T, H, d], is the output before its rounding, for an exact backward."""
-    _, H, d = q.shape
-    G = k.shape[1]
-    _same_dtype(torch.bfloat16, q, k, v, out)
-    _same_dtype(torch.float32, slopes, lse, out_f32)
-    _same_dtype(torch.int32, prefix)
-    T = batch.n_total
-    strides, (pq, pk, pv) = _position_strides(T, H, G, d, q, k, v)
-    _holds(T * H * d, out, out_f32)
-    _holds(T * H, lse)
-    _holds(H, slopes)
-    _holds(batch.n_graphs, prefix)
+    bf16, f32 = torch.bfloat16, torch.float32
+    (_, H, d), G, T = q.shape, k.shape[1], batch.n_total
+    q_shape, kv_shape, n = (T, H, d), (T, G, d), T * H * d
+    (pq, sq), (pk, sk), (pv, sv) = _rows(q, bf16, q_shape), _rows(k, bf16, kv_shape), _rows(v, bf16, kv_shape)
     if workspace is None:
         workspace = _workspace(gt_position_attn_fwd_workspace(batch, H, G, d), q.device)
-    st = lib().gt_position_attn_fwd(pq, pk, pv, _ptr(slopes), _ptr(prefix), batch._c_pair()[1], H, G, d, strides,
-                                    int(causal), float(cap), _ptr(out), _ptr(lse), _ptr(out_f32), _ptr(workspace), workspace.numel(), _stream())
+    st = lib().gt_position_attn_fwd(pq, pk, pv, _dense(slopes, f32, H), _dense(prefix, torch.int32, batch.n_graphs), batch._c_pair()[1], H, G, d,
+                                    _strides(sq, sk, sv), int(causal), float(cap), _dense(out, bf16, n), _dense(lse, f32, T * H),
+                                    _dense(out_f32, f32, n), _ptr(workspace), workspace.numel(), _stream())
     _raise(st, "gt_position_attn_fwd")
     return workspace
 
@@ -602,21 +590,16 @@ def gt_position_attn_bwd(q, k, v, out, dout, lse, slopes: Optional[torch.Tensor]
                          causal: bool, cap: float, dq, dk, dv, out_f32: Optional[torch.Tensor] = None,
                          workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gradients of gt_position_attn_fwd; rows of q, k, v, dq, dk and dv may lie apart.  ``out`` may be None beside ``out_f32``."""
-    _, H, d = q.shape
-    G = k.shape[1]
-    _same_dtype(torch.bfloat16, q, k, v, out, dout, dq, dk, dv)
-    _same_dtype(torch.float32, slopes, lse, out_f32)
-    _same_dtype(torch.int32, prefix)
-    T = batch.n_total
-    strides, (pq, pk, pv, pdq, pdk, pdv) = _position_strides(T, H, G, d, q, k, v, dq, dk, dv)
-    _holds(T * H * d, out, out_f32, dout)
-    _holds(T * H, lse)
-    _holds(H, slopes)
-    _holds(batch.n_graphs, prefix)
+    bf16, f32 = torch.bfloat16, torch.float32
+    (_, H, d), G, T = q.shape, k.shape[1], batch.n_total
+    q_shape, kv_shape, n = (T, H, d), (T, G, d), T * H * d
+    (pq, sq), (pk, sk), (pv, sv) = _rows(q, bf16, q_shape), _rows(k, bf16, kv_shape), _rows(v, bf16, kv_shape)
+    (pdq, sdq), (pdk, sdk), (pdv, sdv) = _rows(dq, bf16, q_shape), _rows(dk, bf16, kv_shape), _rows(dv, bf16, kv_shape)
     if workspace is None:
         workspace = _workspace(gt_position_attn_bwd_workspace(batch, H, G, d), q.device)
-    st = lib().gt_position_attn_bwd(pq, pk, pv, _ptr(out), _ptr(out_f32), _ptr(dout), _ptr(lse), _ptr(slopes), _ptr(prefix), batch._c_pair()[1],
-                                    H, G, d, strides, int(causal), float(cap), pdq, pdk, pdv,
+    st = lib().gt_position_attn_bwd(pq, pk, pv, _dense(out, bf16, n), _dense(out_f32, f32, n), _dense(dout, bf16, n), _dense(lse, f32, T * H),
+                                    _dense(slopes, f32, H), _dense(prefix, torch.int32, batch.n_graphs), batch._c_pair()[1], H, G, d,
+                                    _strides(sq, sk, sv, sdq, sdk, sdv), int(causal), float(cap), pdq, pdk, pdv,
                                     _ptr(workspace), workspace.numel(), _stream())
     _raise(st, "gt_position_attn_bwd")
     return workspace
@@ -625,19 +608,20 @@ def gt_position_attn_bwd(q, k, v, out, dout, lse, slopes: Optional[torch.Tensor]
 def gt_rotary(q, k: Optional[torch.Tensor], frequencies, positions: Optional[torch.Tensor], batch: Batch, interleaved: bool,
               scale: float, inverse: bool, q_out, k_out: Optional[torch.Tensor]) -> None:
     """Rotary positions of q [T, H, d] and k [T, G, d] (or None) by frequencies fp64 [rot_dim / 2]; outputs may be the inputs."""
-    _, H, d = q.shape
-    _same_dtype(q.dtype, k, q_out, k_out)
-    _same_dtype(torch.float64, frequencies)
-    _same_dtype(torch.int32, positions)
-    if q.dtype not in DTYPES:
+    (_, H, d), T, dtype = q.shape, batch.n_total, q.dtype
+    if dtype not in DTYPES:
         raise ValueError("expected bf16, fp16 or fp32")
     if (k is None) != (k_out is None):
         raise ValueError("expected k and k_out, or neither")
-    T, G = batch.n_total, 0 if k is None else k.shape[1]
-    (pq, sq), (pk, sk), (oq, tq), (ok, tk) = (_rows(t, T, G if i % 2 else H, d) for i, t in enumerate((q, k, q_out, k_out)))
-    _holds(T, positions)
-    st = lib().gt_rotary(pq, pk, _ptr(frequencies), _ptr(positions), batch._c_pair()[1], H, G, d,
-                         2 * frequencies.numel(), DTYPES[q.dtype], int(interleaved), float(scale), int(inverse), sq, sk, tq, tk,
+    G, shape = 0, (T, H, d)
+    (pq, sq), (oq, tq) = _rows(q, dtype, shape), _rows(q_out, dtype, shape)
+    pk, sk, ok, tk = None, 0, None, 0
+    if k is not None:
+        G = k.shape[1]
+        shape = (T, G, d)
+        (pk, sk), (ok, tk) = _rows(k, dtype, shape), _rows(k_out, dtype, shape)
+    st = lib().gt_rotary(pq, pk, _dense(frequencies, torch.float64, 0), _dense(positions, torch.int32, T), batch._c_pair()[1], H, G, d,
+                         2 * frequencies.numel(), DTYPES[dtype], int(interleaved), float(scale), int(inverse), sq, sk, tq, tk,
                          oq, ok, _stream())
     _raise(st, "gt_rotary")
 
