@@ -740,6 +740,7 @@ struct PrepareParams {
 // is cleared.  A thread owns a row and adds its products in channel order; the rows reach it through shared memory, because 32 lanes that each walk along a row of their own ask the L1 for every line eight
 // times.  16-byte chunk c of row r lies at chunk c ^ (r & 7): eight neighbouring rows' chunks lie in different banks (D = 32: c ^ (r & 3)).
 constexpr int kPrepareThreads = 256, kPrepareRows = 128;
+constexpr float kLargestTerm = 0x1.fdp127f;      // rounds to a finite bf16
 template <int D>
 __global__ void __launch_bounds__(kPrepareThreads) position_prepare_kernel(const PrepareParams p)
 {
@@ -803,10 +804,10 @@ __global__ void __launch_bounds__(kPrepareThreads) position_prepare_kernel(const
         }
     }
     uint4 e0 = make_uint4(0u, 0u, 0u, 0u), e1 = make_uint4(0u, 0u, 0u, 0u);
-    // A row that is not finite, or belongs to no document, gets zero terms: it may share a 128-row tile with another document's rows.
-    const float l = p.lse[(row % p.n_heads) * p.n_total + row / p.n_heads];
-    if (isfinite(l) && isfinite(acc)) {
-        split3_bf16(-l * p.sqrt_d, e0.x, e0.y);
+    // A row that is not finite, or has terms that bf16 does not hold, gets zero terms: it may share a 128-row tile with another document's rows.
+    const float l = p.lse[(row % p.n_heads) * p.n_total + row / p.n_heads] * p.sqrt_d;
+    if (fabsf(l) < kLargestTerm && fabsf(acc) < kLargestTerm) {
+        split3_bf16(-l, e0.x, e0.y);
         split3_bf16(-acc, e1.x, e1.y);
     }
     p.ext[2 * row] = e0;

@@ -389,3 +389,18 @@ def test_slopes_that_leave_a_query_itself_only(options):
 def test_one_row_of_a_projection():
     """A single token's tensors count as packed, whatever stride their only row has."""
     Case([1], H=4, G=2, seed=29, apart=True).run()
+
+
+@pytest.mark.parametrize("options", [dict(), dict(cap=30.0), dict(slopes=[0.1] * 4)])
+def test_terms_beyond_bf16_of_another_document(options):
+    """dout . out of a row that shares a tile with the document before it is finite in fp32, but not in bf16."""
+    c = Case([100, 28], H=4, G=4, seed=30, **options)
+    gt.gt_check(c.forward())
+    gt.gt_check(c.backward(exact=False))
+    want = [x[:100].clone() for x in (c.dk, c.dv)]
+    c.out[100], c.dout[100] = 0.0, 0.0
+    c.out[100, :, 0], c.out[100, :, 1] = 1.9921875 * 2.0 ** 64, 0.75 * 2.0 ** 57
+    c.dout[100, :, :2] = 2.0 ** 63
+    assert bool((c.out[100].float() * c.dout[100].float()).sum(-1).isfinite().all())
+    gt.gt_check(c.backward(exact=False))
+    assert all(torch.equal(x[:100], y) for x, y in zip((c.dk, c.dv), want))
