@@ -558,6 +558,11 @@ def _strides(*strides):
     return ctypes.byref(_GtRowStrides(*strides)) if any(strides) else None
 
 
+def _output_and_workspace(out_f32, workspace):
+    """``out_f32`` and ``workspace`` in either order: bytes are the workspace, so that it may come at once behind the results, too."""
+    return (workspace, out_f32) if out_f32 is not None and out_f32.dtype is torch.uint8 else (out_f32, workspace)
+
+
 def gt_position_attn_fwd_workspace(batch: Batch, n_heads: int, n_kv_heads: int, head_dim: int) -> int:
     b = batch._c_pair()[1]
     return int(lib().gt_position_attn_fwd_workspace(b, n_heads, n_kv_heads, head_dim))
@@ -567,11 +572,12 @@ def gt_position_attn_fwd(q, k, v, slopes: Optional[torch.Tensor], prefix: Option
                          causal: bool, cap: float, out, lse, out_f32: Optional[torch.Tensor] = None,
                          workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention over token sequences: q [T, H, d], k and v [T, G, d] (rows may lie apart), slopes fp32 [H], prefix int32 [documents];
-    ``out_f32``, fp32 [T, H, d], is the output before its rounding, for an exact backward."""
+    ``out_f32``, fp32 [T, H, d], is the output before its rounding, for an exact backward.  The workspace may also come before it."""
     bf16, f32 = torch.bfloat16, torch.float32
     (_, H, d), G, T = q.shape, k.shape[1], batch.n_total
     q_shape, kv_shape, n = (T, H, d), (T, G, d), T * H * d
     (pq, sq), (pk, sk), (pv, sv) = _rows(q, bf16, q_shape), _rows(k, bf16, kv_shape), _rows(v, bf16, kv_shape)
+    out_f32, workspace = _output_and_workspace(out_f32, workspace)
     if workspace is None:
         workspace = _workspace(gt_position_attn_fwd_workspace(batch, H, G, d), q.device)
     st = lib().gt_position_attn_fwd(pq, pk, pv, _dense(slopes, f32, H), _dense(prefix, torch.int32, batch.n_graphs), batch._c_pair()[1], H, G, d,
@@ -589,12 +595,14 @@ def gt_position_attn_bwd_workspace(batch: Batch, n_heads: int, n_kv_heads: int, 
 def gt_position_attn_bwd(q, k, v, out, dout, lse, slopes: Optional[torch.Tensor], prefix: Optional[torch.Tensor], batch: Batch,
                          causal: bool, cap: float, dq, dk, dv, out_f32: Optional[torch.Tensor] = None,
                          workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """Gradients of gt_position_attn_fwd; rows of q, k, v, dq, dk and dv may lie apart.  ``out`` may be None beside ``out_f32``."""
+    """Gradients of gt_position_attn_fwd; rows of q, k, v, dq, dk and dv may lie apart.  ``out`` may be None beside ``out_f32``.
+    The workspace may also come before ``out_f32``."""
     bf16, f32 = torch.bfloat16, torch.float32
     (_, H, d), G, T = q.shape, k.shape[1], batch.n_total
     q_shape, kv_shape, n = (T, H, d), (T, G, d), T * H * d
     (pq, sq), (pk, sk), (pv, sv) = _rows(q, bf16, q_shape), _rows(k, bf16, kv_shape), _rows(v, bf16, kv_shape)
     (pdq, sdq), (pdk, sdk), (pdv, sdv) = _rows(dq, bf16, q_shape), _rows(dk, bf16, kv_shape), _rows(dv, bf16, kv_shape)
+    out_f32, workspace = _output_and_workspace(out_f32, workspace)
     if workspace is None:
         workspace = _workspace(gt_position_attn_bwd_workspace(batch, H, G, d), q.device)
     st = lib().gt_position_attn_bwd(pq, pk, pv, _dense(out, bf16, n), _dense(out_f32, f32, n), _dense(dout, bf16, n), _dense(lse, f32, T * H),

@@ -404,3 +404,20 @@ def test_terms_beyond_bf16_of_another_document(options):
     assert bool((c.out[100].float() * c.dout[100].float()).sum(-1).isfinite().all())
     gt.gt_check(c.backward(exact=False))
     assert all(torch.equal(x[:100], y) for x, y in zip((c.dk, c.dv), want))
+
+
+@pytest.mark.parametrize("options", [dict(), dict(prefix=[9, 200], cap=20.0, slopes=[0.5, 0.0, 0.1, 1.0])])
+def test_workspace_at_once_behind_the_results(options):
+    """A call without the fp32 output may hand over its workspace where that output would stand."""
+    c = Case([100, 300], H=4, G=2, seed=31, **options)
+    wf = gt._workspace(gt.gt_position_attn_fwd_workspace(c.batch, 4, 2, 64), "cuda")
+    wb = gt._workspace(gt.gt_position_attn_bwd_workspace(c.batch, 4, 2, 64), "cuda")
+    assert gt.gt_position_attn_fwd(c.q, c.k, c.v, c.slopes, c.prefix, c.batch, True, c.cap, c.out, c.lse, wf) is wf
+    assert gt.gt_position_attn_bwd(c.q, c.k, c.v, c.out, c.dout, c.lse, c.slopes, c.prefix, c.batch, True, c.cap, c.dq, c.dk, c.dv, wb) is wb
+    gt.gt_check(wf)
+    gt.gt_check(wb)
+    c.check(exact=False)
+    out32, kept = c.out32.clone(), c.out.clone()
+    gt.gt_position_attn_fwd(c.q, c.k, c.v, c.slopes, c.prefix, c.batch, True, c.cap, c.out, c.lse, wf, c.out32)
+    gt.gt_check(wf)
+    assert not torch.equal(c.out32, out32) and rel_l2(to_f64(c.out), to_f64(kept)) <= 2 * ONE

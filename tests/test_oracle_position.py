@@ -245,3 +245,38 @@ def test_frequencies_refuse_what_leaves_the_range(args):
     with pytest.raises(gt.GtError) as e:
         gt.gt_rotary_frequencies(*args)
     assert e.value.status == 1
+
+
+class _Recorded:
+    """Stands for the library: notes the arguments of the last call and succeeds."""
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.name, self.args = name, args
+            return 0
+        return call
+
+
+@pytest.mark.parametrize("f32,ws", [(False, False), (True, False), (False, True), (True, True)])
+@pytest.mark.parametrize("first", ["workspace", "out_f32", "by name"])
+def test_workspace_and_fp32_output_come_in_either_order(monkeypatch, f32, ws, first):
+    """Behind the results a call has the workspace, the fp32 output or both."""
+    seen = _Recorded()
+    monkeypatch.setattr(gt, "lib", lambda: seen)
+    monkeypatch.setattr(gt, "_stream", lambda: 0)
+    made = _OnGpu(torch.zeros(512, dtype=torch.uint8))
+    monkeypatch.setattr(gt, "_workspace", lambda n, device: made)
+    t = dict(q=_bf16(8, 4, 64), k=_bf16(8, 2, 64), v=_bf16(8, 2, 64), out=_bf16(8, 4, 64), dout=_bf16(8, 4, 64), lse=_OnGpu(torch.zeros(4, 8)),
+             dq=_bf16(8, 4, 64), dk=_bf16(8, 2, 64), dv=_bf16(8, 2, 64))
+    out32 = _OnGpu(torch.zeros(8, 4, 64)) if f32 else None
+    space = _OnGpu(torch.zeros(1024, dtype=torch.uint8)) if ws else None
+    behind = (space, out32) if space is not None else () if out32 is None else (out32,)
+    more, named = {"workspace": (behind, {}), "out_f32": ((out32, space), {}), "by name": ((), {"workspace": space, "out_f32": out32})}[first]
+    want32, used = out32.data_ptr() if f32 else None, space if ws else made
+    got = gt.gt_position_attn_fwd(t["q"], t["k"], t["v"], None, None, gt.Batch(8), True, 0.0, t["out"], t["lse"], *more, **named)
+    assert seen.name == "gt_position_attn_fwd" and got is used
+    assert seen.args[-6:] == (t["out"].data_ptr(), t["lse"].data_ptr(), want32, used.data_ptr(), used.numel(), 0)
+    got = gt.gt_position_attn_bwd(t["q"], t["k"], t["v"], t["out"], t["dout"], t["lse"], None, None, gt.Batch(8), True, 0.0, t["dq"], t["dk"], t["dv"],
+                                  *more, **named)
+    assert seen.name == "gt_position_attn_bwd" and got is used
+    assert seen.args[3:5] == (t["out"].data_ptr(), want32) and seen.args[-3:] == (used.data_ptr(), used.numel(), 0)
