@@ -70,7 +70,8 @@ __device__ __forceinline__ void write_work_list(int4* list, int32_t entries, con
 {
     const int lane = threadIdx.x & 31;
     const int32_t c0 = cu_seqlens[g], n = cu_seqlens[g + 1] - c0, blocks = (n + kRows - 1) / kRows;
-    int32_t first = c0 / kRows + g, end = (c0 + n) / kRows + g + 1;      // in batch order: the next graph's first entry
+    // in batch order: the next graph's first entry, or all that is left (rows may follow the last graph)
+    int32_t first = c0 / kRows + g, end = g == n_graphs - 1 ? entries : (c0 + n) / kRows + g + 1;
     if (n_graphs <= kListSorted) {
         int32_t before = 0, all = 0;
         for (int j = lane; j < n_graphs; j += 32) {

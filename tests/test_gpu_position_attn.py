@@ -421,3 +421,40 @@ def test_workspace_at_once_behind_the_results(options):
     gt.gt_position_attn_fwd(c.q, c.k, c.v, c.slopes, c.prefix, c.batch, True, c.cap, c.out, c.lse, wf, c.out32)
     gt.gt_check(wf)
     assert not torch.equal(c.out32, out32) and rel_l2(to_f64(c.out), to_f64(kept)) <= 2 * ONE
+
+
+def _ragged(n, high, seed):
+    return [int(x) for x in np.random.Generator(np.random.PCG64(seed)).integers(0, high, n)]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("documents", [66, 40])
+def test_work_list_with_rows_behind_the_last_document(documents, causal):
+    """Ragged documents in the order of the batch and by size, so many that both directions work by a list, and several tiles' rows behind them."""
+    Case(_ragged(documents, 900, 32), H=8, G=4, d=32, causal=causal, extra=1500, seed=32).run()
+
+
+def test_work_list_of_a_shorter_batch_in_the_same_workspace_and_graph():
+    """The number of rows stays, the documents get shorter from call to call: what an earlier list said must not be read again."""
+    lengths = _ragged(66, 900, 33)
+    c = Case(lengths, H=8, G=4, d=32, extra=300, seed=33)
+    wf, wb = c.forward(), c.backward()
+    gt.gt_check(wf)
+    gt.gt_check(wb)
+    c.check()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        c.forward(ws=wf)
+        c.backward(ws=wb)
+    for share in (0.6, 0.1):
+        c.cu = np.concatenate([[0], np.cumsum([int(n * share) for n in lengths])]).astype(np.int32)
+        c.n = int(c.cu[-1])
+        c.batch.cu_seqlens.copy_(torch.from_numpy(c.cu))
+        ref = None
+        for again in (lambda: (c.forward(ws=wf), c.backward(ws=wb)), g.replay):
+            for x in (c.out, c.out32, c.lse, c.dq, c.dk, c.dv):
+                x.fill_(LEFT)
+            again()
+            gt.gt_check(wf)
+            gt.gt_check(wb)
+            ref = c.check(ref=ref)
