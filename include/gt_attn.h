@@ -430,10 +430,13 @@ gt_status gt_feature_code_dweights(const float* dtable, const uint32_t* vectors,
  * One document's values never reach another's results.  Within a document a NaN or an infinity in k or v may reach queries that
  * do not see it (they meet it multiplied by zero), as may one in q or dout reach gradients.
  *
- * out_f32: fp32 [T, n_heads, d], or NULL: the output before its rounding, for the backward.  Where a row has few large
- * probabilities, dout . out is subtracted from nearly equal numbers, and the rounding of a bf16 out alone moves dq and dk by half a
- * per cent (scores of standard deviation 4; 0.3 % with out_f32); the forward also forms it with more care (and takes 10 to 30 % longer).
- * The backward takes out (which may be NULL beside an out_f32), out_f32 and lse of the forward with the same arguments.  With P = exp(S - lse), Delta_i = dout_i . out_i:
+ * out_f32: fp32 [T, n_heads, d], or NULL: the output before its rounding, for the backward, which forms Delta_i = dout_i . out_i of it.  (A
+ * rounded output would not do: in rows of few large probabilities Delta is subtracted from nearly equal numbers, and dq and dk were off
+ * by half a per cent and more.)  The forward then divides by the sum of the rounded probabilities, and takes 10 to 30 % longer.  Without
+ * it the backward makes another pass over the pairs for Delta_i = sum_j P_ij (dout_i . v_j), which takes about as long as a forward.  dq and
+ * dk are off by 0.24 % then, with out_f32 by up to 0.29 % in such rows (scores of standard deviation 4).
+ * The backward takes the lse of the forward with the same arguments, its out_f32, or else its out (which may be NULL beside an out_f32, and is
+ * not read).  With P = exp(S - lse):
  *     dv_j = sum P_ij dout_i,   dS_ij = P_ij (dout_i . v_j - Delta_i) (1 - tanh^2(x_ij / cap)),
  *     dq_i = sum_j dS_ij k_j / sqrt(d),   dk_j = sum dS_ij q_i / sqrt(d),
  * dk and dv summed over the query heads that share a key head.  dq, dk, dv (bf16) are overwritten; they must not overlap any

@@ -61,8 +61,8 @@ def scores(q, k, causal, prefix, slopes, cap):
 
 def attention(q, k, v, dout=None, causal=False, prefix=0, slopes=None, cap=0.0):
     """q, dout fp64 [n,H,d]; k, v [n,G,d]; slopes [H].  Returns a dict: out [n,H,d], lse [H,n], with dout dq, dk, dv, and `bounds`, the
-    same keys: elementwise limits of the error (dq and dk: with the forward's fp32 output, `dq_out`, `dk_out` with the bf16 one), and
-    `norms`."""
+    same keys: elementwise limits of the error (dq and dk: with the forward's fp32 output; `dq_own`, `dk_own` where the backward sums Delta itself,
+    from probabilities in fp32; `dq_out`, `dk_out` if it were made of the bf16 output), and `norms`."""
     n, H, d = q.shape
     G = k.shape[1]
     vv, kk = np.repeat(v, H // G, axis=1), np.repeat(k, H // G, axis=1)
@@ -104,6 +104,13 @@ def attention(q, k, v, dout=None, causal=False, prefix=0, slopes=None, cap=0.0):
         off_x = 1.01 * ((HALF_STEP + wrong) * np.abs(dx) + p * (g + 4e-6) * (off_delta + tail) + p * np.abs(dp - delta) * 4e-6)
         b["dq" + key] = _rows_times(off_x, np.abs(kk)) / np.sqrt(d) + HALF_STEP * 1.01 * np.abs(r["dq"]) + 1e-30
         b["dk" + key] = heads(_columns_times(off_x, np.abs(q))) / np.sqrt(d) + HALF_STEP * 1.01 * np.abs(r["dk"]) + 1e-30
+    # Delta of the backward's own probabilities, in fp32: what they are off, less what they have in common, and the sums
+    off_delta = (p * wrong * np.abs(dp - delta)).sum(2, keepdims=True) + (p * tail).sum(2, keepdims=True)
+    off_x = 1.01 * ((HALF_STEP + wrong) * np.abs(dx) + p * (g + 4e-6) * (off_delta + tail) + p * np.abs(dp - delta) * 4e-6)
+    b["dq_own"] = _rows_times(off_x, np.abs(kk)) / np.sqrt(d) + HALF_STEP * 1.01 * np.abs(r["dq"]) + 1e-30
+    b["dk_own"] = heads(_columns_times(off_x, np.abs(q))) / np.sqrt(d) + HALF_STEP * 1.01 * np.abs(r["dk"]) + 1e-30
+    r["norms"]["dq_own"] = MEAN_STEP * np.sqrt(_weighed((dx * dx).transpose(0, 2, 1), kk * kk) / d + squares(r["dq"]))
+    r["norms"]["dk_own"] = MEAN_STEP * np.sqrt(_weighed(dx * dx, q * q) / d + squares(r["dk"]))
     # Delta with the fp32 output: sum_j of (a probability's rounding) P (dP - Delta), since the rounded normaliser takes the mean off
     off_delta2 = ((p * (dp - delta)) ** 2).sum(2)
     pull = _rows_times(p * g, kk)

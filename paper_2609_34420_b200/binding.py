@@ -572,7 +572,7 @@ def gt_position_attn_fwd(q, k, v, slopes: Optional[torch.Tensor], prefix: Option
                          causal: bool, cap: float, out, lse, out_f32: Optional[torch.Tensor] = None,
                          workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention over token sequences: q [T, H, d], k and v [T, G, d] (rows may lie apart), slopes fp32 [H], prefix int32 [documents];
-    ``out_f32``, fp32 [T, H, d], is the output before its rounding, for an exact backward.  The workspace may also come before it."""
+    ``out_f32``, fp32 [T, H, d], is the output before its rounding, which saves the backward a pass.  The workspace may also come before it."""
     bf16, f32 = torch.bfloat16, torch.float32
     (_, H, d), G, T = q.shape, k.shape[1], batch.n_total
     q_shape, kv_shape, n = (T, H, d), (T, G, d), T * H * d

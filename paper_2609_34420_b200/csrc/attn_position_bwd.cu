@@ -29,6 +29,7 @@
 #include <cmath>
 
 #include "attn_position.cuh"
+#include "attn_position_delta.cuh"
 
 namespace gt {
 namespace {
@@ -710,19 +711,8 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     if (warp == 2) tmem_dealloc(tmem, 512);
 }
 
-__device__ __forceinline__ void split3_bf16(float v, uint32_t& w01, uint32_t& w2)
-{
-    const __nv_bfloat16 hi = __float2bfloat16_rn(v);
-    const float r1 = v - __bfloat162float(hi);
-    const __nv_bfloat16 mid = __float2bfloat16_rn(r1);
-    const __nv_bfloat16 lo = __float2bfloat16_rn(r1 - __bfloat162float(mid));
-    w01 = (uint32_t)__bfloat16_as_ushort(hi) | ((uint32_t)__bfloat16_as_ushort(mid) << 16);
-    w2 = (uint32_t)__bfloat16_as_ushort(lo);
-}
-
 struct PrepareParams {
-    const __nv_bfloat16* out;
-    const float* out_f32;      // the forward's output before its rounding, where the caller has it (then instead of `out`)
+    const float* out_f32;      // the forward's output before its rounding; nullptr: another kernel writes -Delta
     const __nv_bfloat16* dout;
     const float* lse;
     uint4* ext;
@@ -740,7 +730,6 @@ struct PrepareParams {
 // is cleared.  A thread owns a row and adds its products in channel order; the rows reach it through shared memory, because 32 lanes that each walk along a row of their own ask the L1 for every line eight
 // times.  16-byte chunk c of row r lies at chunk c ^ (r & 7): eight neighbouring rows' chunks lie in different banks (D = 32: c ^ (r & 3)).
 constexpr int kPrepareThreads = 256, kPrepareRows = 128;
-constexpr float kLargestTerm = 0x1.fdp127f;      // rounds to a finite bf16
 template <int D>
 __global__ void __launch_bounds__(kPrepareThreads) position_prepare_kernel(const PrepareParams p)
 {
@@ -772,19 +761,18 @@ __global__ void __launch_bounds__(kPrepareThreads) position_prepare_kernel(const
     };
     for (size_t i = (size_t)blockIdx.x * kPrepareThreads + threadIdx.x; i < p.n_acc; i += (size_t)p.row_blocks * kPrepareThreads)
         p.acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    stage(s_do, p.dout, Tag<false>{});
-    if (p.out_f32 != nullptr) stage(s_o, p.out_f32, Tag<true>{});
-    else stage(s_o, p.out, Tag<false>{});
-    __syncthreads();
     const int r = (int)threadIdx.x;
-    if (r >= rows) return;
     const size_t row = row0 + r;
     float acc = 0.f;
+    if (p.out_f32 != nullptr) {
+        stage(s_do, p.dout, Tag<false>{});
+        stage(s_o, p.out_f32, Tag<true>{});
+        __syncthreads();
+        if (r >= rows) return;
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i) {
-        const uint4 b = *(const uint4*)(s_do + r * 2 * D + ((i ^ (r & kSwz)) << 4));
-        const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
-        if (p.out_f32 != nullptr) {
+        for (int i = 0; i < kChunks; ++i) {
+            const uint4 b = *(const uint4*)(s_do + r * 2 * D + ((i ^ (r & kSwz)) << 4));
+            const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
             const float4 a0 = *(const float4*)(s_o + r * 4 * D + (((2 * i) ^ (r & kSwz)) << 4));
             const float4 a1 = *(const float4*)(s_o + r * 4 * D + (((2 * i + 1) ^ (r & kSwz)) << 4));
             const float a[8] = {a0.x, a0.y, a0.z, a0.w, a1.x, a1.y, a1.z, a1.w};
@@ -793,16 +781,9 @@ __global__ void __launch_bounds__(kPrepareThreads) position_prepare_kernel(const
                 acc += a[2 * k] * __uint_as_float(bw[k] << 16);
                 acc += a[2 * k + 1] * __uint_as_float(bw[k] & 0xffff0000u);
             }
-        } else {
-            const uint4 a = *(const uint4*)(s_o + r * 2 * D + ((i ^ (r & kSwz)) << 4));
-            const uint32_t aw[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                acc += __uint_as_float(aw[k] << 16) * __uint_as_float(bw[k] << 16);
-                acc += __uint_as_float(aw[k] & 0xffff0000u) * __uint_as_float(bw[k] & 0xffff0000u);
-            }
         }
     }
+    if (r >= rows) return;
     uint4 e0 = make_uint4(0u, 0u, 0u, 0u), e1 = make_uint4(0u, 0u, 0u, 0u);
     // A row that is not finite, or has terms that bf16 does not hold, gets zero terms: it may share a 128-row tile with another document's rows.
     const float l = p.lse[(row % p.n_heads) * p.n_total + row / p.n_heads] * p.sqrt_d;
@@ -975,7 +956,6 @@ extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const vo
     cudaStream_t s = (cudaStream_t)stream;
 
     PrepareParams pre{};
-    pre.out = (const __nv_bfloat16*)out;
     pre.out_f32 = out_f32;
     pre.dout = (const __nv_bfloat16*)dout;
     pre.lse = lse;
@@ -994,6 +974,30 @@ extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const vo
     auto prepare = head_dim == 64 ? position_prepare_kernel<64> : position_prepare_kernel<32>;
     if ((st = launch_overlapped(prepare, dim3(pre.row_blocks + list_blocks), kPrepareThreads, 0, s, pre)) != GT_OK) return st;
 
+    if (out_f32 == nullptr) {
+        DeltaParams d{};
+        d.cu_seqlens = batch->cu_seqlens;
+        d.prefix = prefix;
+        d.slopes = slopes;
+        d.lse = lse;
+        d.ext = pre.ext;
+        d.status = p.status;
+        d.list = p.list;
+        d.n_graphs = batch->n_graphs;
+        d.n_total = T;
+        d.n_heads = n_heads;
+        d.group = p.group;
+        d.causal = p.causal;
+        d.by_work = p.by_work;
+        d.blocks = p.blocks;
+        d.c1 = p.c1;
+        d.to_tanh = p.to_tanh;
+        d.cap2 = p.cap2;
+        st = position::pick(head_dim == 64, cap > 0.f, slopes != nullptr, [&](auto wide, auto capped, auto sloped) {
+            return launch_delta<decltype(wide)::value ? 64 : 32, decltype(capped)::value, decltype(sloped)::value>(maps, d, (unsigned)(p.n_items / p.parts), s);
+        });
+        if (st != GT_OK) return st;
+    }
     st = position::pick(head_dim == 64, cap > 0.f, slopes != nullptr, [&](auto wide, auto capped, auto sloped) {
         return launch<decltype(wide)::value ? 64 : 32, decltype(capped)::value, decltype(sloped)::value>(maps, p, batch, s);
     });
