@@ -983,6 +983,7 @@ extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const vo
         d.ext = pre.ext;
         d.status = p.status;
         d.list = p.list;
+        d.n_items = p.n_items / p.parts;
         d.n_graphs = batch->n_graphs;
         d.n_total = T;
         d.n_heads = n_heads;
@@ -994,7 +995,7 @@ extern "C" gt_status gt_position_attn_bwd(const void* q, const void* k, const vo
         d.to_tanh = p.to_tanh;
         d.cap2 = p.cap2;
         st = position::pick(head_dim == 64, cap > 0.f, slopes != nullptr, [&](auto wide, auto capped, auto sloped) {
-            return launch_delta<decltype(wide)::value ? 64 : 32, decltype(capped)::value, decltype(sloped)::value>(maps, d, (unsigned)(p.n_items / p.parts), s);
+            return launch_delta<decltype(wide)::value ? 64 : 32, decltype(capped)::value, decltype(sloped)::value>(maps, d, s);
         });
         if (st != GT_OK) return st;
     }
