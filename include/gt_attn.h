@@ -439,7 +439,8 @@ gt_status gt_feature_code_dweights(const float* dtable, const uint32_t* vectors,
  * not read).  With P = exp(S - lse):
  *     dv_j = sum P_ij dout_i,   dS_ij = P_ij (dout_i . v_j - Delta_i) (1 - tanh^2(x_ij / cap)),
  *     dq_i = sum_j dS_ij k_j / sqrt(d),   dk_j = sum dS_ij q_i / sqrt(d),
- * dk and dv summed over the query heads that share a key head.  dq, dk, dv (bf16) are overwritten; they must not overlap any
+ * dk and dv summed over the query heads that share a key head.  A Delta_i that is not below 3.38e38 in size (bf16 holds no more) counts as zero:
+ * that query's dq and its share of dk are then wrong, dv is not.  dq, dk, dv (bf16) are overwritten; they must not overlap any
  * input.  dq, and where several thread blocks share a key's queries dk and dv (shared key heads, small batches), are accumulated with
  * floating-point atomics in fp32: their low-order bits may differ from run to run.
  * Workspace as for every call (header zero at first, and calls that may overlap on the GPU need workspaces of their own: their kernels

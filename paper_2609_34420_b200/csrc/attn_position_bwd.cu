@@ -785,12 +785,11 @@ __global__ void __launch_bounds__(kPrepareThreads) position_prepare_kernel(const
     }
     if (r >= rows) return;
     uint4 e0 = make_uint4(0u, 0u, 0u, 0u), e1 = make_uint4(0u, 0u, 0u, 0u);
-    // A row that is not finite, or has terms that bf16 does not hold, gets zero terms: it may share a 128-row tile with another document's rows.
+    // A term that is not finite, or that bf16 does not hold, is taken for zero, each for itself: its row may share a 128-row tile with another
+    // document's rows.
     const float l = p.lse[(row % p.n_heads) * p.n_total + row / p.n_heads] * p.sqrt_d;
-    if (fabsf(l) < kLargestTerm && fabsf(acc) < kLargestTerm) {
-        split3_bf16(-l, e0.x, e0.y);
-        split3_bf16(-acc, e1.x, e1.y);
-    }
+    if (fabsf(l) < kLargestTerm) split3_bf16(-l, e0.x, e0.y);
+    if (fabsf(acc) < kLargestTerm) split3_bf16(-acc, e1.x, e1.y);
     p.ext[2 * row] = e0;
     p.ext[2 * row + 1] = e1;
 }

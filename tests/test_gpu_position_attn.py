@@ -524,3 +524,27 @@ def test_other_documents_values_do_not_leak_without_the_fp32_output(options):
             for name in ("dq", "dk", "dv"):
                 x, y = to_f64(getattr(c, name)[rows]), to_f64(getattr(clean, name)[rows])
                 assert np.isfinite(x).all() and rel_l2(x, y) <= 2 * ONE, name              # (the order of the sums)
+
+
+@pytest.mark.parametrize("exact", [True, False])
+@pytest.mark.parametrize("options", [dict(), dict(cap=30.0), dict(slopes=[0.1] * 4)])
+def test_terms_beyond_bf16_leave_the_rest_of_their_own_document(options, exact):
+    """dout . out of one query overflows: dv does not depend on it, nor do the gradients of queries and heads beside it."""
+    c = Case([100, 28], H=4, G=4, seed=37, **options)
+    gt.gt_check(c.forward())
+    row, big = 110, 2.0 ** 63
+    c.dout[row, 1, :2] = big
+    if exact:
+        c.out32[row, 1, :2] = 2.0 ** 66
+    else:                                                # (the backward's own Delta: sums of dout . v)
+        c.v[100:row + 1, 1, :2] = 2.0 ** 66
+        gt.gt_check(c.forward())
+    gt.gt_check(c.backward(exact))
+    ref, got = c.oracle(), c.results()
+    assert np.all(np.abs(got["dv"] - ref["dv"]) <= ref["bounds"]["dv"])
+    others = [h for h in range(4) if h != 1]
+    for name in ("dq", "dk"):
+        limit = ref["bounds"][name if exact else name + "_own"]
+        assert np.all(np.abs(got[name] - ref[name])[:, others] <= limit[:, others]), name
+        assert np.all(np.abs(got[name] - ref[name])[:100] <= limit[:100]), name
+    assert np.all(np.abs(got["dq"] - ref["dq"])[row + 1:] <= ref["bounds"]["dq" if exact else "dq_own"][row + 1:])
