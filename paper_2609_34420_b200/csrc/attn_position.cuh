@@ -185,6 +185,17 @@ __device__ __forceinline__ bool item_wait(uint32_t bar, uint32_t parity, volatil
     return sm100::mbar_wait(bar, parity, abort_flag, status, site);
 }
 
+// Whether a warp goes on to an item of n rows: not behind the last one (n 0), and not once a wait was given up, its own for the item (`had`) or
+// another warp's.  The flag may be raised between two looks at it, so all that go on together have one look: `any` is true for all of them if
+// it is for one, the lanes of a warp, or the warps that meet in named barriers on the way.  (One that left on its own would be waited for without end.)
+// The warp that fetches the items writes no description any more once it has given up waiting for its place: others may still work by the old one.
+template <typename Any>
+__device__ __forceinline__ bool goes_on(bool had, int32_t n, const volatile uint32_t* abort_flag, Any any)
+{
+    return !any(!had || n <= 0 || *abort_flag != 0u);
+}
+__device__ __forceinline__ bool warp_any(bool x) { return __any_sync(0xffffffffu, x); }
+
 // Rows [first, 128) of a tile in shared memory are cleared by the calling warp, for MMAs that read the tile afterwards: what lies behind
 // a document's last row belongs to another one, and 0 x NaN is NaN.
 __device__ __forceinline__ void clear_rows(uint8_t* tile, int first, int row_bytes)

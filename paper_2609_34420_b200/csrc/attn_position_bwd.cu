@@ -97,7 +97,7 @@ enum Barrier {
     kBarAccFree,                             //      4 warp arrivals: they have been read
     kNumBarriers
 };
-constexpr int kNbDqStaged = 4, kNbDqStagingFree = 5;       // named barriers
+constexpr int kNbDqStaged = 4, kNbDqStagingFree = 5, kNbDqItem = 6;       // named barriers
 
 template <int D>
 struct Smem {
@@ -204,8 +204,8 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 
     // Item number k of this CTA; false: there are no more.  give_back: the calling warp is done with its description.
     auto take = [&](int k) -> bool {
-        item_wait(bar(kBarItemFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 300);
-        return items[k & 1].n > 0 && *abort_flag == 0u;
+        const bool had = item_wait(bar(kBarItemFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 300);
+        return goes_on(had, items[k & 1].n, abort_flag, warp_any);
     };
     auto give_back = [&](int k) {
         __syncwarp();
@@ -266,20 +266,22 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         }
                     }
                 }
-                if (k >= 2) good &= item_wait(bar(kBarItemEmpty + (k & 1)), ((k >> 1) & 1) ^ 1, abort_flag, p.status, 301);
-                if (lane == 0) {
+                if (k >= 2 && good) good = !warp_any(!item_wait(bar(kBarItemEmpty + (k & 1)), ((k >> 1) & 1) ^ 1, abort_flag, p.status, 301));
+                if (good && lane == 0) {
                     items[k & 1] = item;
                     mbar_arrive(bar(kBarItemFull + (k & 1)));
                 }
                 __syncwarp();
                 if (item.n == 0) break;
+                if (!good) continue;
                 const int kv_head = item.head / p.group;
-                if (k >= 2) good &= mbar_wait(bar(kBarKEmpty + (k & 1)), ((k >> 1) & 1) ^ 1, abort_flag, p.status, 302);
+                auto wait = [&](int i, uint32_t parity, uint32_t site) { good = good && !warp_any(!mbar_wait(bar(i), parity, abort_flag, p.status, site)); };
+                if (k >= 2) wait(kBarKEmpty + (k & 1), ((k >> 1) & 1) ^ 1, 302);
                 if (good && lane == 0) {
                     mbar_arrive_expect_tx(bar(kBarKFull + (k & 1)), L::kTileBytes);
                     tma_load_3d(smem_u32(smem + L::kK + (k & 1) * L::kTileBytes), &tmap_k, bar(kBarKFull + (k & 1)), 0, kv_head, item.node0 + item.kv0);
                 }
-                if (k >= 1) good &= mbar_wait(bar(kBarVEmpty), (k - 1) & 1, abort_flag, p.status, 303);
+                if (k >= 1) wait(kBarVEmpty, (k - 1) & 1, 303);
                 if (good && lane == 0) {
                     mbar_arrive_expect_tx(bar(kBarVFull), L::kTileBytes);
                     tma_load_3d(smem_u32(smem + L::kV), &tmap_v, bar(kBarVFull), 0, kv_head, item.node0 + item.kv0);
@@ -287,7 +289,7 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 const int n_q = item.q_tiles();
                 for (int i = 0; i < n_q; ++i, ++c) {
                     const int s = c & 1;
-                    if (c >= 2) good &= mbar_wait(bar(kBarStageEmpty + s), ((c >> 1) & 1) ^ 1, abort_flag, p.status, 310);
+                    if (c >= 2) wait(kBarStageEmpty + s, ((c >> 1) & 1) ^ 1, 310);
                     if (good && lane == 0) {
                         const int32_t row = item.node0 + item.q_lo + i * kTile;
                         mbar_arrive_expect_tx(bar(kBarQdoFull + s), 2 * L::kTileBytes + kExtTileBytes);
@@ -643,7 +645,9 @@ position_bwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         const int r = ((warp & 3) << 5) | lane;
         const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
         int c = 0;
-        for (int k = 0; take(k); ++k) {
+        for (int k = 0;; ++k) {
+            const bool had = item_wait(bar(kBarItemFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 304);
+            if (!goes_on(had, items[k & 1].n, abort_flag, [&](bool x) { return named_barrier_or(kNbDqItem, 128, x); })) break;
             const int n_q = items[k & 1].q_tiles();
             const int32_t n_own = items[k & 1].n - items[k & 1].q_lo, row0 = items[k & 1].node0 + items[k & 1].q_lo, col0 = items[k & 1].head * D;
             for (int i = 0; i < n_q; ++i, ++c) {

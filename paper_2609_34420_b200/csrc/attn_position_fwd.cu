@@ -200,11 +200,12 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 
     // Item number k of this CTA, read by whole warps; false: there are no more.
     auto take = [&](int k, Item& item) -> bool {
-        item_wait(bar(kBarItemFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 200);
+        const bool had = item_wait(bar(kBarItemFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 200);
         item = items[k & 1];
+        if (!goes_on(had, item.n, abort_flag, warp_any)) return false;
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(kBarItemEmpty + (k & 1)));
-        return item.n > 0 && *abort_flag == 0u;
+        return true;
     };
 
     if (warp < 4) {
@@ -213,8 +214,9 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             // ---- the items: the CTA's own number, then what the counter gives, as late as its latency allows: the longest items come
             // first, and who takes the short ones of the end is decided by who is done (two items ahead: causal 16 384 tokens 441 us, now 370) ----
             int32_t index = (int32_t)blockIdx.x;
+            bool good = true;                                // no wait has been given up (then the items are only counted to their end)
             for (int k = 0;; ++k) {
-                if (k > 0) item_wait(bar(kBarFetch), (k - 1) & 1, abort_flag, p.status, 203);
+                if (k > 0 && good) good = !warp_any(!item_wait(bar(kBarFetch), (k - 1) & 1, abort_flag, p.status, 203));
                 Item item{};
                 while (item.n == 0) {
                     if (index < 0) {
@@ -260,8 +262,8 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     if (block >= n_blocks) item.n = 0;
                     else item.prefix = p.prefix ? p.prefix[g] : 0;
                 }
-                if (k >= 2) item_wait(bar(kBarItemEmpty + (k & 1)), ((k >> 1) & 1) ^ 1, abort_flag, p.status, 201);
-                if (lane == 0) {
+                if (k >= 2 && good) good = !warp_any(!item_wait(bar(kBarItemEmpty + (k & 1)), ((k >> 1) & 1) ^ 1, abort_flag, p.status, 201));
+                if (good && lane == 0) {
                     items[k & 1] = item;
                     mbar_arrive(bar(kBarItemFull + (k & 1)));
                 }
@@ -405,8 +407,8 @@ position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         int step0 = 0, own = 0;                 // score tiles, and this query tile's, so far
         for (int k = 0;; ++k) {
         // (the item is read again where its results are written, and given back behind that: fewer registers in between)
-        item_wait(bar(kBarItemFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 202);
-        if (items[k & 1].n == 0 || *abort_flag != 0u) break;
+        const bool had = item_wait(bar(kBarItemFull + (k & 1)), (k >> 1) & 1, abort_flag, p.status, 202);
+        if (!goes_on(had, items[k & 1].n, abort_flag, [&](bool x) { return named_barrier_or(pair_bar, 64, x); })) break;
         Span span;
         span.set(items[k & 1], p.causal);
         const int32_t first = t == 0 ? span.skip : 0, diagonal = span.diagonal, step_by = span.tiles;

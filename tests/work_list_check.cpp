@@ -1,41 +1,6 @@
 // The work lists of packed batches (write_work_list, write_list), run on the CPU with a warp of 32 threads: every entry is written, by all that
 // write it alike, none beyond the end, every block of every graph is there, and what is left says "unused", with and without rows behind the last graph.
-#include <cuda_runtime.h>
-#include <math.h>
-#include <stdint.h>
-#include <stdio.h>
-
-#include <algorithm>
-#include <barrier>
-#include <cstring>
-#include <random>
-#include <thread>
-#include <vector>
-
-// What the device code uses of its compiler, for threads in the place of lanes.
-using std::max;
-using std::min;
-struct Index { unsigned x; };
-static thread_local Index threadIdx, blockIdx, blockDim;
-static std::barrier<> g_step(32);
-static int g_values[32];
-template <typename T> static T __reduce_add_sync(unsigned, T v)
-{
-    g_values[threadIdx.x] = (int)v;
-    g_step.arrive_and_wait();
-    int sum = 0;
-    for (int x : g_values) sum += x;
-    g_step.arrive_and_wait();
-    return (T)sum;
-}
-unsigned __ballot_sync(unsigned, bool);
-int __popc(unsigned);
-unsigned atomicCAS(uint32_t*, unsigned, unsigned);
-size_t __cvta_generic_to_shared(const void*);
-static float __uint_as_float(uint32_t x) { float r; memcpy(&r, &x, 4); return r; }
-static uint32_t __float_as_uint(float x) { uint32_t r; memcpy(&r, &x, 4); return r; }
-
-#include "attn_position.cuh"
+#include "device_on_cpu.h"
 
 struct Batch {
     std::vector<int32_t> cu;
