@@ -290,6 +290,7 @@ extern "C" gt_status gt_rotary_frequencies(int32_t rot_dim, double base, gt_rota
             kept = r <= low ? 0.0 : r >= high ? 1.0 : (r - low) / (high - low);
         }
         frequencies_host[i] = f * ((1.0 - kept) / factor + kept);
+        if (!isfinite(frequencies_host[i])) return GT_ERR_INVALID_ARG;
     }
     return GT_OK;
 }

@@ -280,3 +280,11 @@ def test_workspace_and_fp32_output_come_in_either_order(monkeypatch, f32, ws, fi
                                   *more, **named)
     assert seen.name == "gt_position_attn_bwd" and got is used
     assert seen.args[3:5] == (t["out"].data_ptr(), want32) and seen.args[-3:] == (used.data_ptr(), used.numel(), 0)
+
+
+@pytest.mark.parametrize("args", [(64, 1e-300, "linear", 1e-100), (64, 1e-300, "parts", 1e-100, 1e-290, 1.0, 8.0)])
+def test_frequencies_refuse_a_table_with_an_infinity(args):
+    """Base and factor are in range, but not base^-x / factor."""
+    with pytest.raises(gt.GtError) as e:
+        gt.gt_rotary_frequencies(*args)
+    assert e.value.status == 1
