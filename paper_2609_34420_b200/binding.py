@@ -558,6 +558,20 @@ def _strides(*strides):
     return ctypes.byref(_GtRowStrides(*strides)) if any(strides) else None
 
 
+_devices = None
+
+
+def _on_current_device(*tensors) -> None:
+    """Kernels run on the current device, which another one's memory is out of reach of (a machine with one has nothing to ask)."""
+    global _devices
+    if _devices is None:
+        _devices = torch.cuda.device_count()
+    if _devices > 1:
+        here = _device()
+        if any(t is not None and t.get_device() != here for t in tensors):
+            raise ValueError("expected tensors of the current CUDA device")
+
+
 def _output_and_workspace(out_f32, workspace):
     """``out_f32`` and ``workspace`` in either order: bytes are the workspace, so that it may come at once behind the results, too."""
     return (workspace, out_f32) if out_f32 is not None and out_f32.dtype is torch.uint8 else (out_f32, workspace)
@@ -580,6 +594,7 @@ def gt_position_attn_fwd(q, k, v, slopes: Optional[torch.Tensor], prefix: Option
     out_f32, workspace = _output_and_workspace(out_f32, workspace)
     if workspace is None:
         workspace = _workspace(gt_position_attn_fwd_workspace(batch, H, G, d), q.device)
+    _on_current_device(q, k, v, out, lse, slopes, prefix, out_f32, workspace, batch.cu_seqlens)
     st = lib().gt_position_attn_fwd(pq, pk, pv, _dense(slopes, f32, H), _dense(prefix, torch.int32, batch.n_graphs), batch._c_pair()[1], H, G, d,
                                     _strides(sq, sk, sv), int(causal), float(cap), _dense(out, bf16, n), _dense(lse, f32, T * H),
                                     _dense(out_f32, f32, n), _ptr(workspace), workspace.numel(), _stream())
@@ -605,6 +620,7 @@ def gt_position_attn_bwd(q, k, v, out, dout, lse, slopes: Optional[torch.Tensor]
     out_f32, workspace = _output_and_workspace(out_f32, workspace)
     if workspace is None:
         workspace = _workspace(gt_position_attn_bwd_workspace(batch, H, G, d), q.device)
+    _on_current_device(q, k, v, out, dout, lse, slopes, prefix, dq, dk, dv, out_f32, workspace, batch.cu_seqlens)
     st = lib().gt_position_attn_bwd(pq, pk, pv, _dense(out, bf16, n), _dense(out_f32, f32, n), _dense(dout, bf16, n), _dense(lse, f32, T * H),
                                     _dense(slopes, f32, H), _dense(prefix, torch.int32, batch.n_graphs), batch._c_pair()[1], H, G, d,
                                     _strides(sq, sk, sv, sdq, sdk, sdv), int(causal), float(cap), pdq, pdk, pdv,
@@ -628,6 +644,7 @@ def gt_rotary(q, k: Optional[torch.Tensor], frequencies, positions: Optional[tor
         G = k.shape[1]
         shape = (T, G, d)
         (pk, sk), (ok, tk) = _rows(k, dtype, shape), _rows(k_out, dtype, shape)
+    _on_current_device(q, k, frequencies, positions, q_out, k_out, batch.cu_seqlens)
     st = lib().gt_rotary(pq, pk, _dense(frequencies, torch.float64, 0), _dense(positions, torch.int32, T), batch._c_pair()[1], H, G, d,
                          2 * frequencies.numel(), DTYPES[dtype], int(interleaved), float(scale), int(inverse), sq, sk, tq, tk,
                          oq, ok, _stream())

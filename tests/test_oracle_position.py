@@ -288,3 +288,50 @@ def test_frequencies_refuse_a_table_with_an_infinity(args):
     with pytest.raises(gt.GtError) as e:
         gt.gt_rotary_frequencies(*args)
     assert e.value.status == 1
+
+
+def _calls(monkeypatch, **other):
+    """One call of each binding on tensors that pass for ones on the GPU, with some replaced; the library only notes what it gets."""
+    seen = _Recorded()
+    monkeypatch.setattr(gt, "lib", lambda: seen)
+    monkeypatch.setattr(gt, "_stream", lambda: 0)
+    a = dict(q=_bf16(8, 4, 64), k=_bf16(8, 2, 64), v=_bf16(8, 2, 64), out=_bf16(8, 4, 64), dout=_bf16(8, 4, 64), lse=_OnGpu(torch.zeros(4, 8)),
+             slopes=_OnGpu(torch.zeros(4)), prefix=_OnGpu(torch.zeros(1, dtype=torch.int32)), batch=gt.Batch(8), causal=True, cap=0.0, dq=_bf16(8, 4, 64),
+             dk=_bf16(8, 2, 64), dv=_bf16(8, 2, 64), out_f32=_OnGpu(torch.zeros(8, 4, 64)), workspace=_OnGpu(torch.zeros(256, dtype=torch.uint8)))
+    r = dict(q=a["q"], k=a["k"], frequencies=_OnGpu(torch.ones(32, dtype=torch.float64)), positions=_OnGpu(torch.zeros(8, dtype=torch.int32)),
+             batch=a["batch"], interleaved=False, scale=1.0, inverse=False, q_out=_bf16(8, 4, 64), k_out=_bf16(8, 2, 64))
+    a, r = a | {x: other[x] for x in other if x in a}, r | {x: other[x] for x in other if x in r}
+    fwd = {x: a[x] for x in a if x not in ("dout", "dq", "dk", "dv")}
+    return seen, (lambda: gt.gt_position_attn_fwd(**fwd)), (lambda: gt.gt_position_attn_bwd(**a)), (lambda: gt.gt_rotary(**r))
+
+
+def _on(device, t):
+    t.get_device = lambda: device
+    return t
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v", "out", "dout", "lse", "slopes", "prefix", "dq", "dk", "dv", "out_f32", "workspace", "frequencies", "positions",
+                                  "q_out", "k_out", "cu_seqlens"])
+def test_bindings_refuse_tensors_of_another_device(monkeypatch, name):
+    monkeypatch.setattr(gt, "_device", lambda: 1)
+    monkeypatch.setattr(_OnGpu, "get_device", lambda self: 1, raising=False)
+    monkeypatch.setattr(gt, "_devices", 2)
+    seen, *calls = _calls(monkeypatch)
+    for call in calls:
+        call()
+    made = {"lse": _OnGpu(torch.zeros(4, 8)), "slopes": _OnGpu(torch.zeros(4)), "prefix": _OnGpu(torch.zeros(1, dtype=torch.int32)),
+            "out_f32": _OnGpu(torch.zeros(8, 4, 64)), "workspace": _OnGpu(torch.zeros(256, dtype=torch.uint8)),
+            "frequencies": _OnGpu(torch.ones(32, dtype=torch.float64)), "positions": _OnGpu(torch.zeros(8, dtype=torch.int32))}
+    far = _on(0, made.get(name) or _bf16(8, 4 if name in ("q", "out", "dout", "dq", "q_out") else 2, 64))
+    if name == "cu_seqlens":
+        seen, *calls = _calls(monkeypatch, batch=gt.Batch(8, 1, 8, _on(0, _OnGpu(torch.tensor([0, 8], dtype=torch.int32)))))
+    else:
+        seen, *calls = _calls(monkeypatch, **{name: far})
+    refused = 0
+    for call in calls:
+        try:
+            call()
+        except ValueError:
+            refused += 1
+    both, forward, rotary = ("q", "k", "cu_seqlens"), ("v", "out", "lse", "slopes", "prefix", "out_f32", "workspace"), ("frequencies", "positions", "q_out", "k_out")
+    assert refused == (3 if name in both else 2 if name in forward else 1), refused
