@@ -572,6 +572,13 @@ def _on_current_device(*tensors) -> None:
             raise ValueError("expected tensors of the current CUDA device")
 
 
+def _lse(t: torch.Tensor, H: int, T: int) -> Optional[int]:
+    """Address of the rows' log-sum-exp: [H, T] (a longer row would leave every head but the first out of place), or as many values without a shape."""
+    if t is not None and t.dim() == 2 and t.shape[1] != T:
+        raise ValueError(f"expected a tensor [{H}, {T}]")
+    return _dense(t, torch.float32, T * H)
+
+
 def _output_and_workspace(out_f32, workspace):
     """``out_f32`` and ``workspace`` in either order: bytes are the workspace, so that it may come at once behind the results, too."""
     return (workspace, out_f32) if out_f32 is not None and out_f32.dtype is torch.uint8 else (out_f32, workspace)
@@ -596,7 +603,7 @@ def gt_position_attn_fwd(q, k, v, slopes: Optional[torch.Tensor], prefix: Option
         workspace = _workspace(gt_position_attn_fwd_workspace(batch, H, G, d), q.device)
     _on_current_device(q, k, v, out, lse, slopes, prefix, out_f32, workspace, batch.cu_seqlens)
     st = lib().gt_position_attn_fwd(pq, pk, pv, _dense(slopes, f32, H), _dense(prefix, torch.int32, batch.n_graphs), batch._c_pair()[1], H, G, d,
-                                    _strides(sq, sk, sv), int(causal), float(cap), _dense(out, bf16, n), _dense(lse, f32, T * H),
+                                    _strides(sq, sk, sv), int(causal), float(cap), _dense(out, bf16, n), _lse(lse, H, T),
                                     _dense(out_f32, f32, n), _ptr(workspace), workspace.numel(), _stream())
     _raise(st, "gt_position_attn_fwd")
     return workspace
@@ -621,7 +628,7 @@ def gt_position_attn_bwd(q, k, v, out, dout, lse, slopes: Optional[torch.Tensor]
     if workspace is None:
         workspace = _workspace(gt_position_attn_bwd_workspace(batch, H, G, d), q.device)
     _on_current_device(q, k, v, out, dout, lse, slopes, prefix, dq, dk, dv, out_f32, workspace, batch.cu_seqlens)
-    st = lib().gt_position_attn_bwd(pq, pk, pv, _dense(out, bf16, n), _dense(out_f32, f32, n), _dense(dout, bf16, n), _dense(lse, f32, T * H),
+    st = lib().gt_position_attn_bwd(pq, pk, pv, _dense(out, bf16, n), _dense(out_f32, f32, n), _dense(dout, bf16, n), _lse(lse, H, T),
                                     _dense(slopes, f32, H), _dense(prefix, torch.int32, batch.n_graphs), batch._c_pair()[1], H, G, d,
                                     _strides(sq, sk, sv, sdq, sdk, sdv), int(causal), float(cap), pdq, pdk, pdv,
                                     _ptr(workspace), workspace.numel(), _stream())

@@ -335,3 +335,13 @@ def test_bindings_refuse_tensors_of_another_device(monkeypatch, name):
             refused += 1
     both, forward, rotary = ("q", "k", "cu_seqlens"), ("v", "out", "lse", "slopes", "prefix", "out_f32", "workspace"), ("frequencies", "positions", "q_out", "k_out")
     assert refused == (3 if name in both else 2 if name in forward else 1), refused
+
+
+def test_bindings_refuse_an_lse_with_longer_rows(monkeypatch):
+    """Rows behind the batch's belong to q and the results, not to lse, whose heads lie n_total apart."""
+    seen, fwd_call, bwd_call, _ = _calls(monkeypatch, lse=_OnGpu(torch.zeros(4, 9)), q=_bf16(9, 4, 64), out=_bf16(9, 4, 64), out_f32=_OnGpu(torch.zeros(9, 4, 64)))
+    for call in (fwd_call, bwd_call):
+        with pytest.raises(ValueError):
+            call()
+    seen, fwd_call, bwd_call, _ = _calls(monkeypatch, lse=_OnGpu(torch.zeros(40)))
+    fwd_call(), bwd_call()
