@@ -579,6 +579,12 @@ def _lse(t: torch.Tensor, H: int, T: int) -> Optional[int]:
     return _dense(t, torch.float32, T * H)
 
 
+def _cap(cap) -> float:
+    """As a float; one that fp32 would take for 0, which means no cap, is as little in range as any other below 1e-6."""
+    cap = float(cap)
+    return cap if cap == 0.0 or abs(cap) > 1e-30 else float("nan")
+
+
 def _output_and_workspace(out_f32, workspace):
     """``out_f32`` and ``workspace`` in either order: bytes are the workspace, so that it may come at once behind the results, too."""
     return (workspace, out_f32) if out_f32 is not None and out_f32.dtype is torch.uint8 else (out_f32, workspace)
@@ -603,7 +609,7 @@ def gt_position_attn_fwd(q, k, v, slopes: Optional[torch.Tensor], prefix: Option
         workspace = _workspace(gt_position_attn_fwd_workspace(batch, H, G, d), q.device)
     _on_current_device(q, k, v, out, lse, slopes, prefix, out_f32, workspace, batch.cu_seqlens)
     st = lib().gt_position_attn_fwd(pq, pk, pv, _dense(slopes, f32, H), _dense(prefix, torch.int32, batch.n_graphs), batch._c_pair()[1], H, G, d,
-                                    _strides(sq, sk, sv), int(causal), float(cap), _dense(out, bf16, n), _lse(lse, H, T),
+                                    _strides(sq, sk, sv), int(causal), _cap(cap), _dense(out, bf16, n), _lse(lse, H, T),
                                     _dense(out_f32, f32, n), _ptr(workspace), workspace.numel(), _stream())
     _raise(st, "gt_position_attn_fwd")
     return workspace
@@ -630,7 +636,7 @@ def gt_position_attn_bwd(q, k, v, out, dout, lse, slopes: Optional[torch.Tensor]
     _on_current_device(q, k, v, out, dout, lse, slopes, prefix, dq, dk, dv, out_f32, workspace, batch.cu_seqlens)
     st = lib().gt_position_attn_bwd(pq, pk, pv, _dense(out, bf16, n), _dense(out_f32, f32, n), _dense(dout, bf16, n), _lse(lse, H, T),
                                     _dense(slopes, f32, H), _dense(prefix, torch.int32, batch.n_graphs), batch._c_pair()[1], H, G, d,
-                                    _strides(sq, sk, sv, sdq, sdk, sdv), int(causal), float(cap), pdq, pdk, pdv,
+                                    _strides(sq, sk, sv, sdq, sdk, sdv), int(causal), _cap(cap), pdq, pdk, pdv,
                                     _ptr(workspace), workspace.numel(), _stream())
     _raise(st, "gt_position_attn_bwd")
     return workspace

@@ -345,3 +345,16 @@ def test_bindings_refuse_an_lse_with_longer_rows(monkeypatch):
             call()
     seen, fwd_call, bwd_call, _ = _calls(monkeypatch, lse=_OnGpu(torch.zeros(40)))
     fwd_call(), bwd_call()
+
+
+@pytest.mark.parametrize("cap", [1e-46, -1e-60, 5e-324])
+def test_a_cap_that_fp32_takes_for_none_is_out_of_range(monkeypatch, cap):
+    assert fwd(cap=math.nan) == 1 and bwd(cap=math.nan) == 1
+    seen, fwd_call, bwd_call, _ = _calls(monkeypatch, cap=cap)
+    fwd_call()
+    assert math.isnan(seen.args[11])
+    bwd_call()
+    assert math.isnan(seen.args[15])
+    seen, fwd_call, bwd_call, _ = _calls(monkeypatch, cap=-0.0)
+    fwd_call()
+    assert seen.args[11] == 0.0
