@@ -41,6 +41,7 @@
 #include <math.h>
 
 #include "attn_common.cuh"
+#include "attn_terms.cuh"
 #include "sm100_primitives.cuh"
 
 namespace gt {
@@ -698,16 +699,6 @@ __device__ __forceinline__ void transpose_tile(const uint8_t* __restrict__ spd, 
     }
 }
 
-__device__ __forceinline__ void split3_bf16(float v, uint32_t& w01, uint32_t& w2)
-{
-    const __nv_bfloat16 hi = __float2bfloat16_rn(v);
-    const float r1 = v - __bfloat162float(hi);
-    const __nv_bfloat16 mid = __float2bfloat16_rn(r1);
-    const __nv_bfloat16 lo = __float2bfloat16_rn(r1 - __bfloat162float(mid));
-    w01 = (uint32_t)__bfloat16_as_ushort(hi) | ((uint32_t)__bfloat16_as_ushort(mid) << 16);
-    w2 = (uint32_t)__bfloat16_as_ushort(lo);
-}
-
 struct PrepareParams {
     const uint8_t* spd;
     uint8_t* spd_t;
@@ -832,13 +823,10 @@ __global__ void __launch_bounds__(kPrepareThreads) bwd_prepare_kernel(const __gr
     }
     uint4 e0 = make_uint4(0u, 0u, 0u, 0u), e1 = make_uint4(0u, 0u, 0u, 0u);
     // A row whose forward state is not final on this rank (a ring step's context holds lse = -inf for the rows
-    // of other ranks) gets zero terms: the row may share a 128-row tile with rows that are used, where its columns
+    // of other ranks) gets a zero term: the row may share a 128-row tile with rows that are used, where its columns
     // are masked by assignment after the exponential, and a non-finite term would turn 0 * (dP - Delta) into NaN.
-    const float l = p.lse[(row % p.n_heads) * p.n_total + row / p.n_heads];
-    if (isfinite(l) && isfinite(acc)) {
-        split3_bf16(-l * p.sqrt_d, e0.x, e0.y);
-        split3_bf16(-acc, e1.x, e1.y);
-    }
+    fold_term(-p.lse[(row % p.n_heads) * p.n_total + row / p.n_heads] * p.sqrt_d, e0.x, e0.y);
+    fold_term(-acc, e1.x, e1.y);
     p.ext[2 * row] = e0;
     p.ext[2 * row + 1] = e1;
 }

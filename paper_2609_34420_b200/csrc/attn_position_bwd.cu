@@ -30,6 +30,7 @@
 
 #include "attn_position.cuh"
 #include "attn_position_delta.cuh"
+#include "attn_terms.cuh"
 
 namespace gt {
 namespace {
@@ -789,11 +790,8 @@ __global__ void __launch_bounds__(kPrepareThreads) position_prepare_kernel(const
     }
     if (r >= rows) return;
     uint4 e0 = make_uint4(0u, 0u, 0u, 0u), e1 = make_uint4(0u, 0u, 0u, 0u);
-    // A term that is not finite, or that bf16 does not hold, is taken for zero, each for itself: its row may share a 128-row tile with another
-    // document's rows.
-    const float l = p.lse[(row % p.n_heads) * p.n_total + row / p.n_heads] * p.sqrt_d;
-    if (fabsf(l) < kLargestTerm) split3_bf16(-l, e0.x, e0.y);
-    if (fabsf(acc) < kLargestTerm) split3_bf16(-acc, e1.x, e1.y);
+    fold_term(-p.lse[(row % p.n_heads) * p.n_total + row / p.n_heads] * p.sqrt_d, e0.x, e0.y);
+    fold_term(-acc, e1.x, e1.y);
     p.ext[2 * row] = e0;
     p.ext[2 * row + 1] = e1;
 }

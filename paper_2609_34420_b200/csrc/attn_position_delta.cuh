@@ -16,6 +16,7 @@
 #pragma once
 
 #include "attn_position.cuh"
+#include "attn_terms.cuh"
 
 namespace gt {
 namespace {
@@ -39,18 +40,6 @@ struct DeltaParams {
 };
 
 constexpr int kDeltaThreads = 640, kDeltaWarps = 16, kDeltaStages = 3;
-constexpr float kLargestTerm = 0x1.fdp127f;      // rounds to a finite bf16
-
-__device__ __forceinline__ void split3_bf16(float v, uint32_t& w01, uint32_t& w2)
-{
-    const __nv_bfloat16 hi = __float2bfloat16_rn(v);
-    const float r1 = v - __bfloat162float(hi);
-    const __nv_bfloat16 mid = __float2bfloat16_rn(r1);
-    const __nv_bfloat16 lo = __float2bfloat16_rn(r1 - __bfloat162float(mid));
-    w01 = (uint32_t)__bfloat16_as_ushort(hi) | ((uint32_t)__bfloat16_as_ushort(mid) << 16);
-    w2 = (uint32_t)__bfloat16_as_ushort(lo);
-}
-
 template <int D>
 struct DeltaSmem {
     static constexpr int kRowBytes = D * 2, kTileBytes = 128 * kRowBytes, kPair = 2 * kTileBytes;
@@ -209,7 +198,7 @@ position_delta_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
                 const float2* of = sums + (k & 1) * 512 + r;
                 const float delta = (of[0].x + of[128].x + of[256].x + of[384].x) / (of[0].y + of[128].y + of[256].y + of[384].y);
                 uint4 e = make_uint4(0u, 0u, 0u, 0u);
-                if (fabsf(delta) < kLargestTerm) split3_bf16(-delta, e.x, e.y);       // (a NaN, too, would reach the rows that share a tile)
+                fold_term(-delta, e.x, e.y);
                 if (it.q0 + r < it.n) p.ext[2 * ((size_t)(it.node0 + it.q0 + r) * p.n_heads + it.head) + 1] = e;
             }
             __syncwarp();

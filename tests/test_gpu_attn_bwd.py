@@ -390,3 +390,21 @@ def test_kernel_event_hook_records_the_main_kernel_of_the_next_calls_only():
     gt.gt_profile_bwd_kernel_events([], [])
     inner = [a.elapsed_time(b) for a, b in zip(before, after)]
     assert all(0.0 < x < t0.elapsed_time(t1) for x in inner), inner
+
+
+@pytest.mark.parametrize("d", [32, 64])
+def test_terms_beyond_bf16_of_another_graph(d):
+    """dout . out of a row that shares a tile with the graph before it is finite in fp32, but not in bf16: that graph's gradients stay as they
+    are, and the row's own graph keeps its dv, which does not depend on it."""
+    case = DeviceCase(wl.small_workload([100, 28], 4, d, 6, seed=21, avg_degree=2.0))
+    out, lse = case.forward()
+    dout = case.dout.clone()
+    dout[100, :, :2] = 2.0 ** 63
+    want = case.backward(out, lse, dout=dout)
+    out[100] = 0.0
+    out[100, :, 0], out[100, :, 1] = 1.9921875 * 2.0 ** 64, 0.75 * 2.0 ** 57
+    assert bool((out[100].float() * dout[100].float()).sum(-1).isfinite().all())
+    got = case.backward(out, lse, dout=dout)
+    for x, y in list(zip(got[:3], want[:3])) + [(got[2][100:], want[2][100:])]:
+        n = 100 if x.shape[0] == 128 else 28
+        assert np.isfinite(to_f64(x[:n])).all() and rel_l2(to_f64(x[:n]), to_f64(y[:n])) <= 2.0 ** -8
