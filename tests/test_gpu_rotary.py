@@ -145,3 +145,26 @@ def test_offsets_beyond_32_bits(rot):
     gt.gt_rotary(q, None, f.cuda(), None, gt.Batch(T), True, 1.0, False, out, None)
     check(q[-9:], out[-9:], f, np.arange(T - 9, T), True, 1.0, False)
     assert not out[:-9].any()
+
+
+@pytest.mark.parametrize("interleaved", [True, False])
+@pytest.mark.parametrize("rot", [64, 6])
+def test_far_positions_within_the_derived_error_of_their_angles(interleaved, rot):
+    """The angle w is off by 3 x 2^-53 w (three roundings in fp64) and, reduced to half a turn at most, by 2^-25 pi (its rounding to fp32); sine and
+    cosine by two units in the last place, 2 x 2^-24; then two products and a sum, 2^-24 each of no more than |a| + |b|."""
+    rng = np.random.Generator(np.random.PCG64(5))
+    position = np.concatenate([[0, 1, -1, (1 << 31) - 1, -(1 << 31)], rng.integers(-(1 << 31), 1 << 31, 300), rng.integers(0, 1 << 20, 300)])
+    T, d = len(position), 64
+    q, k = make(T, 2, 1, d, torch.float32, 4)
+    f = gt.gt_rotary_frequencies(rot, 500000.0)
+    oq, ok = torch.empty_like(q), torch.empty_like(k)
+    p = torch.from_numpy(position.astype(np.int32)).cuda()
+    gt.gt_rotary(q, k, f.cuda(), p, gt.Batch(T), interleaved, 1.0, False, oq, ok)
+    angle = np.abs(position[:, None] * f.numpy()[None, :])
+    slip = 3 * 2.0 ** -53 * angle + 2.0 ** -25 * np.pi + 2 * 2.0 ** -24 + 3 * 2.0 ** -24
+    for x, y in ((q, oq), (k, ok)):
+        x, y = to_f64(x), to_f64(y)
+        off = np.abs(y - opos.rotate(x, f.numpy(), position, interleaved))
+        a, b = (slice(0, rot, 2), slice(1, rot, 2)) if interleaved else (slice(0, rot // 2), slice(rot // 2, rot))
+        limit = (np.abs(x[..., a]) + np.abs(x[..., b])) * slip[:, None, :]
+        assert np.all(off[..., a] <= limit) and np.all(off[..., b] <= limit), float(max((off[..., a] / limit).max(), (off[..., b] / limit).max()))
