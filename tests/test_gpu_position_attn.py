@@ -548,3 +548,44 @@ def test_terms_beyond_bf16_leave_the_rest_of_their_own_document(options, exact):
         assert np.all(np.abs(got[name] - ref[name])[:, others] <= limit[:, others]), name
         assert np.all(np.abs(got[name] - ref[name])[:100] <= limit[:100]), name
     assert np.all(np.abs(got["dq"] - ref["dq"])[row + 1:] <= ref["bounds"]["dq" if exact else "dq_own"][row + 1:])
+
+
+@pytest.mark.parametrize("options", [dict(cap=30.0), dict(cap=200.0), dict(slopes=[0.5, 0.1, 0.0, -0.5]), dict(prefix=[70, 150, 100]), dict(causal=False, cap=10.0),
+                                     dict(causal=False, slopes=[0.5, 0.1, 0.0, 1.0]), dict(prefix=[3, 300, 299], cap=50.0, slopes=[0.5, 0.1, 0.0, 1.0])])
+@pytest.mark.parametrize("d", [32, 64])
+def test_other_documents_values_do_not_leak_with_options(options, d):
+    """As above, with caps (one that bounds the scores, one that does not), penalties and prefixes, in a batch that works by the list, too."""
+    kw = dict(lengths=[70, 200, 300], H=4, G=2, d=d, extra=40, seed=38, spread=2.0) | options
+    clean = Case(**kw)
+    clean.run()
+    for bad in (float("nan"), float("inf")):
+        c = Case(**kw)
+        for x in (c.q, c.k, c.v, c.dout):
+            x[70:270] = bad
+            x[570:] = -bad
+        gt.gt_check(c.forward())
+        c.lse[:, 70:270] = bad
+        c.out32[70:270] = bad
+        gt.gt_check(c.backward())
+        for rows in (slice(0, 70), slice(270, 570)):
+            assert torch.equal(c.out[rows], clean.out[rows]) and torch.equal(c.lse[:, rows], clean.lse[:, rows])
+            for name in ("dq", "dk", "dv"):
+                x, y = to_f64(getattr(c, name)[rows]), to_f64(getattr(clean, name)[rows])
+                assert np.isfinite(x).all() and rel_l2(x, y) <= 2 * ONE, name              # (the order of the sums)
+        assert bool((c.out[570:] == LEFT).all()) and bool((c.dk[570:] == LEFT).all())
+
+
+@pytest.mark.parametrize("exact", [True, False])
+@pytest.mark.parametrize("prefix", [1, 129, 700, 1500, 2300])
+def test_shared_key_tiles_with_a_prefix_and_rows_apart(prefix, exact):
+    """One head of a long document: several items share a key tile's queries, from the prefix's beginning or from the tile on."""
+    c = Case([2300], H=1, G=1, prefix=[prefix], extra=60, seed=39, apart=True, spread=2.0)
+    gt.gt_check(c.forward(exact))
+    gt.gt_check(c.backward(exact))
+    c.check(exact)
+    if not exact:
+        _check_own_sums(c, c.oracle())
+
+
+def test_shared_key_tiles_of_several_documents_with_options():
+    Case([1300, 0, 900], H=2, G=1, prefix=[400, 5, 900], slopes=[0.1, 0.5], cap=20.0, extra=200, seed=40, apart=True, spread=3.0).run()
