@@ -558,11 +558,12 @@ def _strides(*strides):
     return ctypes.byref(_GtRowStrides(*strides)) if any(strides) else None
 
 
-_devices = None
+_devices = None      # of this machine; not asked yet
 
 
 def _on_current_device(*tensors) -> None:
-    """Kernels run on the current device, which another one's memory is out of reach of (a machine with one has nothing to ask)."""
+    """Kernels run on the current device, which another one's memory is out of reach of (a machine with one has nothing to ask:
+    callers look at ``_devices`` first)."""
     global _devices
     if _devices is None:
         _devices = torch.cuda.device_count()
@@ -574,15 +575,14 @@ def _on_current_device(*tensors) -> None:
 
 def _lse(t: torch.Tensor, H: int, T: int) -> Optional[int]:
     """Address of the rows' log-sum-exp: [H, T] (a longer row would leave every head but the first out of place), or as many values without a shape."""
-    if t is not None and t.dim() == 2 and t.shape[1] != T:
+    if t is not None and t.dim() == 2 and t.size(1) != T:
         raise ValueError(f"expected a tensor [{H}, {T}]")
     return _dense(t, torch.float32, T * H)
 
 
 def _cap(cap) -> float:
-    """As a float; one that fp32 would take for 0, which means no cap, is as little in range as any other below 1e-6."""
-    cap = float(cap)
-    return cap if cap == 0.0 or abs(cap) > 1e-30 else float("nan")
+    """A cap other than 0 as a float; one that fp32 would take for 0, which means no cap, is as little in range as any other below 1e-6."""
+    return float(cap) if abs(cap) > 1e-30 else float("nan")
 
 
 def _output_and_workspace(out_f32, workspace):
@@ -607,9 +607,10 @@ def gt_position_attn_fwd(q, k, v, slopes: Optional[torch.Tensor], prefix: Option
     out_f32, workspace = _output_and_workspace(out_f32, workspace)
     if workspace is None:
         workspace = _workspace(gt_position_attn_fwd_workspace(batch, H, G, d), q.device)
-    _on_current_device(q, k, v, out, lse, slopes, prefix, out_f32, workspace, batch.cu_seqlens)
+    if _devices != 1:
+        _on_current_device(q, k, v, out, lse, slopes, prefix, out_f32, workspace, batch.cu_seqlens)
     st = lib().gt_position_attn_fwd(pq, pk, pv, _dense(slopes, f32, H), _dense(prefix, torch.int32, batch.n_graphs), batch._c_pair()[1], H, G, d,
-                                    _strides(sq, sk, sv), int(causal), _cap(cap), _dense(out, bf16, n), _lse(lse, H, T),
+                                    _strides(sq, sk, sv), int(causal), _cap(cap) if cap else 0.0, _dense(out, bf16, n), _lse(lse, H, T),
                                     _dense(out_f32, f32, n), _ptr(workspace), workspace.numel(), _stream())
     _raise(st, "gt_position_attn_fwd")
     return workspace
@@ -633,10 +634,11 @@ def gt_position_attn_bwd(q, k, v, out, dout, lse, slopes: Optional[torch.Tensor]
     out_f32, workspace = _output_and_workspace(out_f32, workspace)
     if workspace is None:
         workspace = _workspace(gt_position_attn_bwd_workspace(batch, H, G, d), q.device)
-    _on_current_device(q, k, v, out, dout, lse, slopes, prefix, dq, dk, dv, out_f32, workspace, batch.cu_seqlens)
+    if _devices != 1:
+        _on_current_device(q, k, v, out, dout, lse, slopes, prefix, dq, dk, dv, out_f32, workspace, batch.cu_seqlens)
     st = lib().gt_position_attn_bwd(pq, pk, pv, _dense(out, bf16, n), _dense(out_f32, f32, n), _dense(dout, bf16, n), _lse(lse, H, T),
                                     _dense(slopes, f32, H), _dense(prefix, torch.int32, batch.n_graphs), batch._c_pair()[1], H, G, d,
-                                    _strides(sq, sk, sv, sdq, sdk, sdv), int(causal), _cap(cap), pdq, pdk, pdv,
+                                    _strides(sq, sk, sv, sdq, sdk, sdv), int(causal), _cap(cap) if cap else 0.0, pdq, pdk, pdv,
                                     _ptr(workspace), workspace.numel(), _stream())
     _raise(st, "gt_position_attn_bwd")
     return workspace
@@ -657,7 +659,8 @@ def gt_rotary(q, k: Optional[torch.Tensor], frequencies, positions: Optional[tor
         G = k.shape[1]
         shape = (T, G, d)
         (pk, sk), (ok, tk) = _rows(k, dtype, shape), _rows(k_out, dtype, shape)
-    _on_current_device(q, k, frequencies, positions, q_out, k_out, batch.cu_seqlens)
+    if _devices != 1:
+        _on_current_device(q, k, frequencies, positions, q_out, k_out, batch.cu_seqlens)
     st = lib().gt_rotary(pq, pk, _dense(frequencies, torch.float64, 0), _dense(positions, torch.int32, T), batch._c_pair()[1], H, G, d,
                          2 * frequencies.numel(), DTYPES[dtype], int(interleaved), float(scale), int(inverse), sq, sk, tq, tk,
                          oq, ok, _stream())
