@@ -589,3 +589,35 @@ def test_shared_key_tiles_with_a_prefix_and_rows_apart(prefix, exact):
 
 def test_shared_key_tiles_of_several_documents_with_options():
     Case([1300, 0, 900], H=2, G=1, prefix=[400, 5, 900], slopes=[0.1, 0.5], cap=20.0, extra=200, seed=40, apart=True, spread=3.0).run()
+
+
+def test_captured_and_on_two_streams_without_the_fp32_output():
+    """The pass for Delta in a graph that is replayed on other inputs, and twice at once with workspaces of their own."""
+    c = Case(_ragged(40, 400, 41), H=8, G=8, d=32, spread=4.0, extra=200, seed=41)
+    wf, wb = c.forward(exact=False), c.backward(exact=False)
+    gt.gt_check(wb)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        c.forward(exact=False, ws=wf)
+        c.backward(exact=False, ws=wb)
+    other = Case(_ragged(40, 400, 41), H=8, G=8, d=32, spread=4.0, extra=200, seed=42)
+    for x in ("q", "k", "v", "dout"):
+        getattr(c, x).copy_(getattr(other, x))
+    for x in (c.out, c.lse, c.dq, c.dk, c.dv):
+        x.fill_(LEFT)
+    g.replay()
+    gt.gt_check(wf)
+    gt.gt_check(wb)
+    _check_own_sums(c, c.oracle())
+    a, b = Case([700, 100, 300], H=4, G=2, spread=4.0, seed=43), Case([512, 33], H=8, G=8, cap=10.0, spread=3.0, seed=44)
+    torch.cuda.synchronize()
+    streams, spaces = (torch.cuda.Stream(), torch.cuda.Stream()), []
+    for _ in range(3):
+        for x, s in zip((a, b), streams):
+            with torch.cuda.stream(s):
+                spaces += [x.forward(exact=False), x.backward(exact=False)]
+    torch.cuda.synchronize()
+    for ws in spaces:
+        gt.gt_check(ws)
+    for x in (a, b):
+        _check_own_sums(x, x.oracle())
