@@ -7,8 +7,8 @@
 // dV += P^T dO and dK += dS^T Q; dS^T is also written to shared memory (MN-major A operand) for dQ_i = dS K, which is added to an fp32
 // accumulator in global memory.  A mask is a range of queries for every key, so a thread compares column numbers with two bounds.
 //
-// The per-query terms are folded into the MMAs: a pre-pass writes for every (query, head) a row of 16 bf16 with -lse sqrt(d) and
-// -Delta, each split into three bf16 terms (24 mantissa bits); one extra K = 16 step against a constant tile of ones adds them.  With
+// The per-query terms are folded into the MMAs: a pre-pass (without the forward's fp32 output another one, attn_position_delta.cuh, for Delta) writes for
+// every (query, head) a row of 16 bf16 with -lse sqrt(d) and -Delta, each split into three bf16 terms (24 mantissa bits); one extra K = 16 step against a constant tile of ones adds them.  With
 // capped scores the tanh comes between the product and lse, so that only Delta is folded and lse is read from shared memory.
 //
 // A query tile is two halves of 64 queries with a TMEM stage, MMAs and barriers of their own; while one half's MMAs run, the other
@@ -731,7 +731,7 @@ struct PrepareParams {
 };
 
 // What the main kernel wants done before it, in one launch.  Row blocks: for every row (t, h), ext[t][h][0..2] = three-term bf16 split of
-// -lse sqrt(d), ext[t][h][8..10] = that of -Delta, Delta = sum_c dO[t,h,c] O[t,h,c], zeros elsewhere; and their share of the accumulators
+// -lse sqrt(d), ext[t][h][8..10] = that of -Delta, Delta = sum_c dO[t,h,c] O[t,h,c] (without the fp32 O: zeros, for position_delta_kernel), zeros elsewhere; and their share of the accumulators
 // is cleared.  A thread owns a row and adds its products in channel order; the rows reach it through shared memory, because 32 lanes that each walk along a row of their own ask the L1 for every line eight
 // times.  16-byte chunk c of row r lies at chunk c ^ (r & 7): eight neighbouring rows' chunks lie in different banks (D = 32: c ^ (r & 3)).
 constexpr int kPrepareThreads = 256, kPrepareRows = 128;

@@ -46,7 +46,8 @@ constexpr float kSumThreshold = 0x1p24f;       // tile row sum above which the r
 constexpr float kBoundedCap = 50.0f, kLeastBoundedCap = 0.01f;       // (below, the scaled coefficients leave fp32)
 // Every eighth pair of exponentials is a polynomial's (ex2_pair), which takes load off the special-function unit (77 % busy without) and adds
 // to the issue slots: 16 384 tokens, 8 heads of 64, all pairs 768 -> 710 us (every sixth 746, every fourth 749, every third 790), causal 372 ->
-// 344, causal with the fp32 output 428 -> 409; with the penalty on distance 411 -> 407, and with both 457 -> 475, so not there.
+// 344, causal with the fp32 output 428 -> 409; with the penalty on distance 411 -> 407, and with both 457 -> 475, so not there.  (Back to back, at the
+// 1.76 GHz that the power limit leaves; a few passes at 1 965 MHz: causal 303.)
 constexpr int kEx2Every = 8;
 constexpr float kPeekReach = 24.0f;            // log2 units within which a row's first scores leave the starting reference as it is
 
@@ -145,7 +146,7 @@ __device__ __forceinline__ void setmaxnreg_dec_56() { asm volatile("setmaxnreg.d
 // kExact (with the fp32 output): O is divided by the sum of the probabilities as the MMA reads them, rounded to bf16, so that their
 // rounding cancels where a row has few large ones; lse is that of the unrounded ones all the same.  The backward subtracts dout . out from
 // dout . v_j, two nearly equal numbers in such rows: with scores of standard deviation 4, dq was off by 0.6 % (out rounded to bf16 and
-// divided by the unrounded sum), by 0.45 % without either, and by 0.27 % with both.
+// divided by the unrounded sum), by 0.45 % without either, and by 0.27 % with both.  (A backward without it makes Delta itself: attn_position_delta.cuh.)
 template <int D, int kCapForm, bool kSlope, int kTiles, bool kExact>
 __global__ void __launch_bounds__(128 + 256 * kTiles, 1)
 position_fwd_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,

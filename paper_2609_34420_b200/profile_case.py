@@ -10,7 +10,7 @@ self-contained timing command line for one entry point at a time.  featN times t
 variant on N nodes (H=8, d=64) with VECTORS distinct feature vectors (default 12): the path for any
 features, and the code matrix through the tensor-core kernels of the bucket form.  seqN times a layer
 on a causal document of N tokens (H=8, d=64): rotary positions, attention forward (with the fp32 output that
-its backward takes) and backward, with scores capped at CAP if given.
+its backward takes) and backward, with that output and without, with scores capped at CAP if given.
 """
 from __future__ import annotations
 
@@ -108,6 +108,7 @@ def sequence_timings(n: int, reps: int, cap: float) -> dict:
     res["fwd_f32_ms"] = timed_ms(lambda: gt.gt_position_attn_fwd(qr, kr, v, None, None, batch, True, cap, out, lse, out32, ws_f), reps)
     ws_b = gt.gt_position_attn_bwd(qr, kr, v, out, do, lse, None, None, batch, True, cap, dq, dk, dv, out32)
     res["bwd_ms"] = timed_ms(lambda: gt.gt_position_attn_bwd(qr, kr, v, out, do, lse, None, None, batch, True, cap, dq, dk, dv, out32, ws_b), reps)
+    res["bwd_own_ms"] = timed_ms(lambda: gt.gt_position_attn_bwd(qr, kr, v, out, do, lse, None, None, batch, True, cap, dq, dk, dv, None, ws_b), reps)
     gt.gt_check(ws_f)
     gt.gt_check(ws_b)
     return res
@@ -116,7 +117,7 @@ def sequence_timings(n: int, reps: int, cap: float) -> dict:
 def sequence_case(n: int, reps: int, cap: float) -> int:
     r = sequence_timings(n, reps, cap)
     print(f"rotary {r['rotary_ms']:.4f} ms  {r['rotary_bytes'] / r['rotary_ms'] / 1e6:.1f} GB/s")
-    for name, flops in (("fwd", "fwd_flops"), ("fwd_f32", "fwd_flops"), ("bwd", "bwd_flops")):
+    for name, flops in (("fwd", "fwd_flops"), ("fwd_f32", "fwd_flops"), ("bwd", "bwd_flops"), ("bwd_own", "bwd_flops")):
         print(f"position attention {name} {r[name + '_ms']:.3f} ms  {r[flops] / r[name + '_ms'] / 1e9:.1f} TFLOP/s")
     return 0
 
