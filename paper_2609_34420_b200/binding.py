@@ -206,7 +206,7 @@ try:
     _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
     _stream = lambda: _raw_stream(_device())      # noqa: E731
 except AttributeError:
-    _stream = _public_stream
+    _stream, _device = _public_stream, torch.cuda.current_device
 
 
 def _raise(status: int, where: str) -> None:

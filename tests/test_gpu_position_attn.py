@@ -431,13 +431,13 @@ def _ragged(n, high, seed):
 @pytest.mark.parametrize("documents", [66, 40])
 def test_work_list_with_rows_behind_the_last_document(documents, causal):
     """Ragged documents in the order of the batch and by size, so many that both directions work by a list, and several tiles' rows behind them."""
-    Case(_ragged(documents, 900, 32), H=8, G=4, d=32, causal=causal, extra=1500, seed=32).run()
+    Case(_ragged(documents, 900, 32), H=4 if documents > 64 else 8, G=4, d=32, causal=causal, extra=1500, seed=32).run()
 
 
 def test_work_list_of_a_shorter_batch_in_the_same_workspace_and_graph():
     """The number of rows stays, the documents get shorter from call to call: what an earlier list said must not be read again."""
     lengths = _ragged(66, 900, 33)
-    c = Case(lengths, H=8, G=4, d=32, extra=300, seed=33)
+    c = Case(lengths, H=4, G=2, d=32, extra=300, seed=33)
     wf, wb = c.forward(), c.backward()
     gt.gt_check(wf)
     gt.gt_check(wb)
@@ -621,3 +621,22 @@ def test_captured_and_on_two_streams_without_the_fp32_output():
         gt.gt_check(ws)
     for x in (a, b):
         _check_own_sums(x, x.oracle())
+
+
+@pytest.mark.parametrize("options", [dict(), dict(causal=False), dict(cap=30.0), dict(causal=False, cap=1000.0)])
+def test_slopes_that_leave_a_query_itself_only_without_the_fp32_output(options):
+    """Delta is then dP itself, to the rounding of a quotient: what is left of their difference has the elementwise bound."""
+    c = Case([300, 150], H=4, G=4, slopes=[1e3, 1e9, 1e20, 1e27], seed=45, **options)
+    gt.gt_check(c.forward(exact=False))
+    gt.gt_check(c.backward(exact=False))
+    ref, got = c.check(exact=False, names=("out", "lse", "dv")), c.results()
+    for name in ("dq", "dk"):
+        assert np.all(np.abs(got[name] - ref[name]) <= ref["bounds"][name + "_own"]), name
+
+
+@pytest.mark.parametrize("options", [dict(), dict(cap=30.0, spread=4.0), dict(causal=False), dict(causal=False, cap=10.0), dict(prefix=[200], cap=50.0)])
+def test_slopes_of_either_sign_without_the_fp32_output(options):
+    c = Case([500], H=4, G=4, slopes=[-0.5, 0.5, -3.0, 0.0], seed=46, **options)
+    gt.gt_check(c.forward(exact=False))
+    gt.gt_check(c.backward(exact=False))
+    _check_own_sums(c, c.oracle())
